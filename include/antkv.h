@@ -13,6 +13,13 @@
  *   antkv_gather_rows    copy the selected FP16 rows into the anchor store
  *   antkv_decode_attn    decode attention over codes + FP16 anchors    (Sec. 2.1 Attn; Sec. 3.2 last par.)
  *   antkv_decode_attn_static   the same with scratch inside the library, for callers that cannot allocate
+ * and, for a server whose prompts arrive in chunks beside requests that decode, the FP16 cache that a prompt lives in until
+ * it is encoded:
+ *   antkv_page_map       block tables and slot maps of a step, from the lengths of its requests
+ *   antkv_page_store     new K / V rows to their slots
+ *   antkv_page_attn      attention of each request's new tokens (one to thousands) over its pages, with row statistics
+ *   antkv_page_load      a sequence's rows out of the pages, dense, as antkv_anchor_select and antkv_encode read them
+ *   antkv_prefill_attn_window   prompt attention in which a query sees a window of recent keys and a few first ones
  *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless stated otherwise.  The caller owns all
@@ -271,6 +278,87 @@ int antkv_append_token(const antkv_geom* geom, const void* k_new, const void* v_
  */
 int antkv_prefill_attn(const antkv_geom* geom, const void* q, const void* k, const void* v, int64_t N, int64_t Nq,
                        float scale, void* out, float* row_max, float* row_sum, void* stream);
+
+/*
+ * The same with a sliding window: the query at position p sees keys j <= p with j > p - window (the last `window` positions,
+ * its own among them) or j < n_sink (the first tokens of the context, which stay visible).  window >= 1, n_sink >= 0; either may
+ * exceed N.  K or V that a query does not see has no influence on its row, whatever it holds, infinities and NaN among it.
+ * N up to 2^30.  Otherwise as antkv_prefill_attn.
+ */
+int antkv_prefill_attn_window(const antkv_geom* geom, const void* q, const void* k, const void* v, int64_t N, int64_t Nq,
+                              float scale, int64_t window, int64_t n_sink, void* out, float* row_max, float* row_sum,
+                              void* stream);
+
+/*
+ * A paged FP16 cache.  K and V are two pools fp16 [n_pages][Hkv][page_size][D] (16-byte aligned) that many requests share;
+ * page_size is 16, 32, 64, 128 or 256.  Position j of request r is row j % page_size of page table[r][j / page_size], table being
+ * int32 [R][table_cap]; its slot number is page * page_size + j % page_size, and n_pages * page_size must be below 2^31,
+ * table_cap * page_size at most 2^30.  Lengths, tables and slots live on the device and are read when the kernels run: a captured
+ * step can be replayed with other lengths as long as its sizes (R, T, table_cap) hold them.  Page numbers outside [0, n_pages) and slots outside
+ * the pool are never followed.  These calls read B, Hq, Hkv and D of the geometry; d_sub and n_centroids are not used but must be valid.
+ */
+
+/*
+ * Block tables and slot maps of a step.  Request r has held_len[r] tokens in its pages and gets new_len[r] more (both int32
+ * [R], >= 0, smaller values count as 0; R <= 8192); their rows follow each other in a packed batch of T rows, request by request.
+ *
+ *   table      int32 [R][table_cap]: entries 0 .. ceil(held_len / page_size) - 1 of a row are read where needed and kept; the pages that
+ *              its new tokens need beyond them are taken from free_pages and written behind.  Other entries are left alone.
+ *   free_pages int32 [n_free]: pages that nobody holds, taken in order (request by request) from entry free_at[0] on
+ *              (device int32; NULL = 0)
+ *   ctx_len    int32 [R]: held_len + new_len;   q_start int32 [R + 1]: first row of each request, then the end of the last one
+ *   slot       int32 [T]: slot of each row; -1 for rows behind the last request and for tokens without a page
+ *   status     int32 [2]: the first entry of free_pages that is still free (n_free if there were not enough), and the number of
+ *              requests with new tokens that found no room: the free list, the table row or the batch was too short, or the page that
+ *              they go on in is none.  Table entries that no page was left for hold -1.
+ * Outputs must not overlap inputs (status may not be free_at, ctx_len neither length array); to go on without the host, pass one step's
+ * status as the next one's free_at, ctx_len as held_len, and a second pair of arrays as outputs.
+ * Errors: EINVAL, EUNSUPPORTED (page_size, R), ELAUNCH.
+ */
+int antkv_page_map(int64_t R, const int32_t* held_len, const int32_t* new_len, int32_t* table, int64_t table_cap, int64_t n_pages,
+                   int32_t page_size, const int32_t* free_pages, int64_t n_free, const int32_t* free_at, int64_t T,
+                   int32_t* ctx_len, int32_t* q_start, int32_t* slot, int32_t* status, void* stream);
+
+/*
+ * Row t of k and v (fp16 [T][Hkv][D], both with element strides xs_t, xs_h, channel stride 1; 16-byte aligned, strides multiples of
+ * 8) goes to slot[t] of the pools.  Rows whose slot is negative or behind the pool are skipped.  Slots of one call are distinct:
+ * a slot that is given twice holds pieces of either row.  T == 0 is a no-op.  Errors: EINVAL, EUNSUPPORTED, ELAUNCH.
+ */
+int antkv_page_store(const antkv_geom* geom, const void* k, const void* v, int64_t xs_t, int64_t xs_h, int64_t T,
+                     const int32_t* slot, void* k_pages, void* v_pages, int64_t n_pages, int32_t page_size, void* stream);
+
+/*
+ * Positions first .. first + N - 1 of B requests (geom->B rows of the table) out of the pools: row t of k and v, [B][Hkv][N][D] with element
+ * strides xs_b, xs_h, xs_t (multiples of 8, xs_t >= D), is position first + t.  Rows at or behind ctx_len[b] (int32 [B]; NULL: no
+ * limit) and rows of pages that are none are left as they are.  first + N <= table_cap * page_size.
+ * N == 0 is a no-op.  Errors: EINVAL, EUNSUPPORTED, ELAUNCH.
+ */
+int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_pages, int64_t n_pages, int32_t page_size,
+                    const int32_t* table, int64_t table_cap, const int32_t* ctx_len, int64_t first, int64_t N, void* k, void* v,
+                    int64_t xs_b, int64_t xs_h, int64_t xs_t, void* stream);
+
+/*
+ * Attention of a step's new tokens over the paged cache, in which their own K and V are stored already.  geom->B = R requests; rows
+ * q_start[r] .. q_start[r + 1] - 1 of the packed batch are the LAST positions of request r's ctx_len[r] tokens: row q_start[r] + i stands
+ * at position ctx_len[r] - n + i (n its number of rows) and sees keys j up to its own position; with window >= 1 only those
+ * with j > position - window or j < n_sink (window 0: no limit, at most 2^30).  Any mix of requests with no, one or thousands of rows.
+ *
+ *   q        fp16 [T][Hq][D] with element strides qs_t, qs_h (multiples of 8), 16-byte aligned
+ *   q_start  int32 [R + 1] ascending from 0;  ctx_len int32 [R];  table as above
+ *   out      fp16 [T][Hq][D]; accumulation is fp32, rounded once; probabilities enter the value product rounded to fp16
+ *   row_max, row_sum  optional fp32 [Hq][T] (both or neither) as antkv_prefill_attn's: for a single request the layout that
+ *            antkv_anchor_select takes with Nq = T
+ * Rows of T behind q_start[R] are left as they are.  Keys on pages that are none, and positions behind the table's end, are not
+ * seen; a row that sees nothing is zero, with row_max -inf and row_sum 0.  What a row does not see has no influence on it, whatever it
+ * holds (pages need not be cleared).  Sums have a fixed order: equal inputs give equal bits.
+ * The workspace size is a function of Hq, Hkv, R and T; calls that share a workspace must not overlap.
+ * Errors: EINVAL, EUNSUPPORTED, EWORKSPACE, ELAUNCH.
+ */
+size_t antkv_page_attn_workspace(const antkv_geom* geom, int64_t T);
+int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t qs_h, int64_t T, const int32_t* q_start,
+                    const int32_t* ctx_len, const int32_t* table, int64_t table_cap, const void* k_pages, const void* v_pages,
+                    int64_t n_pages, int32_t page_size, float scale, int64_t window, int64_t n_sink, void* out, float* row_max,
+                    float* row_sum, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * One iteration of the offline token-weighted k-means that learns a codebook (Sec. 3.1, "Offline Token-Aware

@@ -16,6 +16,7 @@ EXPORTS = (
     "antkv_version", "antkv_strerror", "antkv_encode", "antkv_anchor_select_workspace", "antkv_anchor_select",
     "antkv_topk_workspace", "antkv_topk", "antkv_gather_rows", "antkv_decode_attn_workspace", "antkv_decode_attn",
     "antkv_decode_attn_static", "antkv_set_decode_options", "antkv_decode_attn_prerope_workspace", "antkv_decode_attn_prerope", "antkv_append_token", "antkv_prefill_attn", "antkv_kmeans_step_workspace", "antkv_kmeans_step",
+    "antkv_prefill_attn_window", "antkv_page_map", "antkv_page_store", "antkv_page_load", "antkv_page_attn_workspace", "antkv_page_attn",
 )
 
 
@@ -107,6 +108,19 @@ def load_library():
         lib.antkv_decode_attn_prerope.restype = ctypes.c_int
         lib.antkv_decode_attn_prerope.argtypes = [gp, vp, f32, vp, vp, i64, i64, vp, vp, vp, vp, i64, vp, vp, i64,
                                                   f32, ctypes.c_int, i64, vp, vp, sz, vp]
+        i32 = ctypes.c_int32
+        lib.antkv_prefill_attn_window.restype = ctypes.c_int
+        lib.antkv_prefill_attn_window.argtypes = [gp, vp, vp, vp, i64, i64, f32, i64, i64, vp, vp, vp, vp]
+        lib.antkv_page_map.restype = ctypes.c_int
+        lib.antkv_page_map.argtypes = [i64, vp, vp, vp, i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+        lib.antkv_page_store.restype = ctypes.c_int
+        lib.antkv_page_store.argtypes = [gp, vp, vp, i64, i64, i64, vp, vp, vp, i64, i32, vp]
+        lib.antkv_page_load.restype = ctypes.c_int
+        lib.antkv_page_load.argtypes = [gp, vp, vp, i64, i32, vp, i64, vp, i64, i64, vp, vp, i64, i64, i64, vp]
+        lib.antkv_page_attn_workspace.restype = sz
+        lib.antkv_page_attn_workspace.argtypes = [gp, i64]
+        lib.antkv_page_attn.restype = ctypes.c_int
+        lib.antkv_page_attn.argtypes = [gp, vp, i64, i64, i64, vp, vp, vp, i64, vp, vp, i64, i32, f32, i64, i64, vp, vp, vp, vp, sz, vp]
         _lib = lib
     return _lib
 
@@ -387,3 +401,166 @@ def decode_attn_static(geom: Geometry, q: torch.Tensor, scale: float, codes_k: t
         _p(idx_v) if k_v else None, _p(rows_v) if k_v else None, k_v, _p(out), _stream(q))
     _check(rc, "antkv_decode_attn_static")
     return out
+
+
+# ---- the FP16 cache in pages, and windowed prompts ----------------------------------------------------------------------
+
+def _same_device(first: torch.Tensor, **others):
+    """Every tensor on the first one's device, which is made current for the launch if it is not: the returned number, or None."""
+    at = first.get_device()
+    for name, t in others.items():
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"{name} must be on the device of the other tensors")
+    return None if torch.cuda.current_device() == at else at
+
+
+def _launch(call, what: str, device, *args):
+    if device is None:
+        _check(call(*args), what)
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args), what)
+
+
+def _rows(t: torch.Tensor, name: str, heads: int):
+    """fp16 [T, heads, D] with contiguous channels; any strides of tokens and heads."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype is not torch.float16:
+        raise TypeError(f"{name} must be torch.float16")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128 or t.stride(2) != 1:
+        raise ValueError(f"{name} must be [T, {heads}, 128] with contiguous channels")
+
+
+def _pools(k_pages: torch.Tensor, v_pages: torch.Tensor, heads: int):
+    _need(k_pages, torch.float16, "k_pages")
+    _need(v_pages, torch.float16, "v_pages")
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.shape[1] != heads or k_pages.shape[3] != 128:
+        raise ValueError(f"k_pages and v_pages must be [n_pages, {heads}, page_size, 128]")
+    return k_pages.shape[0], k_pages.shape[2]
+
+
+def _ints(t: torch.Tensor, name: str, *shape):
+    _need(t, torch.int32, name)
+    if t.dim() != len(shape) or any(n is not None and t.shape[i] != n for i, n in enumerate(shape)):
+        raise ValueError(f"{name} must be int32 {list('*' if n is None else n for n in shape)}")
+
+
+def prefill_attn_window(geom: Geometry, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, window: int, n_sink: int = 0,
+                        want_stats: bool = True):
+    """antkv_prefill_attn_window: prefill_attn in which a query sees the last `window` positions and the first `n_sink`.
+    q fp16 [B,Hq,Nq,D], k / v fp16 [B,Hkv,N,D] -> (out fp16 [B,Hq,Nq,D], row_max, row_sum)."""
+    _need(q, torch.float16, "q")
+    _need(k, torch.float16, "k")
+    _need(v, torch.float16, "v")
+    B, Hq, Nq, D = q.shape
+    N = k.shape[2]
+    if (B, Hq, D) != (geom.B, geom.Hq, geom.D) or k.shape != (B, geom.Hkv, N, D) or v.shape != k.shape:
+        raise ValueError("q, k and v do not fit the geometry")
+    device = _same_device(q, k=k, v=v)
+    out = torch.empty((B, Hq, Nq, D), dtype=torch.float16, device=q.device)
+    row_max = torch.empty((B, Hq, Nq), dtype=torch.float32, device=q.device) if want_stats else None
+    row_sum = torch.empty((B, Hq, Nq), dtype=torch.float32, device=q.device) if want_stats else None
+    _launch(load_library().antkv_prefill_attn_window, "antkv_prefill_attn_window", device, geom._c, _p(q), _p(k), _p(v), N, Nq, float(scale),
+            int(window), int(n_sink), _p(out), _p(row_max), _p(row_sum), _stream(q))
+    return out, row_max, row_sum
+
+
+def page_map(held_len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor, page_size: int, n_pages: int, free_pages: torch.Tensor,
+             T: int, free_at: torch.Tensor | None = None, out=None):
+    """antkv_page_map: held_len, new_len int32 [R], table int32 [R,cap] (new entries are written), free_pages int32 [n] ->
+    (ctx_len int32 [R], q_start int32 [R+1], slot int32 [T], status int32 [2]).  `out`: such a tuple, to be written again."""
+    R = held_len.shape[0]
+    _ints(held_len, "held_len", R)
+    _ints(new_len, "new_len", R)
+    _ints(table, "table", R, None)
+    _ints(free_pages, "free_pages", None)
+    if free_at is not None:
+        _need(free_at, torch.int32, "free_at")
+        if free_at.numel() < 1:
+            raise ValueError("free_at must hold a number")
+    dev = table.device
+    if out is None:
+        out = tuple(torch.empty(n, dtype=torch.int32, device=dev) for n in (R, R + 1, T, 2))
+    else:
+        for t, name, n in zip(out, ("ctx_len", "q_start", "slot", "status"), (R, R + 1, T, 2)):
+            _ints(t, name, n)
+    ctx_len, q_start, slot, status = out
+    device = _same_device(table, held_len=held_len, new_len=new_len, free_pages=free_pages, free_at=free_at, ctx_len=ctx_len, q_start=q_start,
+                          slot=slot, status=status)
+    _launch(load_library().antkv_page_map, "antkv_page_map", device, R, _p(held_len), _p(new_len), _p(table), table.shape[1], n_pages, page_size,
+            _p(free_pages), free_pages.shape[0], _p(free_at), T, _p(ctx_len), _p(q_start), _p(slot), _p(status), _stream(table))
+    return out
+
+
+def page_store(geom: Geometry, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor) -> None:
+    """antkv_page_store: rows of k, v fp16 [T,Hkv,D] (equal strides, channels contiguous) to slot int32 [T] of the pools
+    fp16 [n_pages,Hkv,page_size,D]."""
+    _rows(k, "k", geom.Hkv)
+    _rows(v, "v", geom.Hkv)
+    n_pages, page_size = _pools(k_pages, v_pages, geom.Hkv)
+    T = k.shape[0]
+    if v.shape[0] != T or (T > 1 and v.stride(0) != k.stride(0)) or (geom.Hkv > 1 and v.stride(1) != k.stride(1)):
+        raise ValueError("k and v must have the same shape and strides")
+    _ints(slot, "slot", T)
+    device = _same_device(k_pages, v_pages=v_pages, k=k, v=v, slot=slot)
+    _launch(load_library().antkv_page_store, "antkv_page_store", device, geom._c, _p(k), _p(v), k.stride(0) if T > 1 else 0,
+            k.stride(1) if geom.Hkv > 1 else 0, T, _p(slot), _p(k_pages), _p(v_pages), n_pages, page_size, _stream(k_pages))
+
+
+def page_load(geom: Geometry, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, N: int, first: int = 0,
+              ctx_len: torch.Tensor | None = None, k: torch.Tensor | None = None, v: torch.Tensor | None = None):
+    """antkv_page_load: positions first .. first + N - 1 of the table's requests -> (k, v) fp16 [B,Hkv,N,D].  Rows at or behind
+    ctx_len (int32 [B]) are left as they are: zeros where k and v are made here."""
+    n_pages, page_size = _pools(k_pages, v_pages, geom.Hkv)
+    _ints(table, "table", geom.B, None)
+    if ctx_len is not None:
+        _ints(ctx_len, "ctx_len", geom.B)
+    shape = (geom.B, geom.Hkv, N, geom.D)
+    if k is None:
+        k = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
+    if v is None:
+        v = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
+    for t, name in ((k, "k"), (v, "v")):
+        _need(t, torch.float16, name)
+        if t.shape != shape:
+            raise ValueError(f"{name} must be {list(shape)}")
+    device = _same_device(k_pages, v_pages=v_pages, table=table, ctx_len=ctx_len, k=k, v=v)
+    _launch(load_library().antkv_page_load, "antkv_page_load", device, geom._c, _p(k_pages), _p(v_pages), n_pages, page_size, _p(table),
+            table.shape[1], _p(ctx_len), first, N, _p(k), _p(v), geom.Hkv * N * geom.D, N * geom.D, geom.D, _stream(k_pages))
+    return k, v
+
+
+def page_attn_workspace(geom: Geometry, T: int, device) -> torch.Tensor:
+    """A workspace of antkv_page_attn_workspace(geom, T) bytes for page_attn, for calls that follow each other on one stream."""
+    return _workspace(load_library().antkv_page_attn_workspace(geom._c, T), device)
+
+
+def page_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Tensor, ctx_len: torch.Tensor, table: torch.Tensor,
+              k_pages: torch.Tensor, v_pages: torch.Tensor, window: int = 0, n_sink: int = 0, out: torch.Tensor | None = None,
+              want_stats: bool = False, workspace: torch.Tensor | None = None):
+    """antkv_page_attn: q fp16 [T,Hq,D] (channels contiguous), q_start int32 [R+1], ctx_len int32 [R], table int32 [R,cap], pools
+    fp16 [n_pages,Hkv,page_size,D], geom.B = R -> (out fp16 [T,Hq,D], row_max, row_sum fp32 [Hq,T] or None).
+    Rows of out behind q_start[R] are left as they are (undefined where out is made here)."""
+    _rows(q, "q", geom.Hq)
+    n_pages, page_size = _pools(k_pages, v_pages, geom.Hkv)
+    T, R = q.shape[0], geom.B
+    _ints(q_start, "q_start", R + 1)
+    _ints(ctx_len, "ctx_len", R)
+    _ints(table, "table", R, None)
+    dev = q.device
+    if out is None:
+        out = torch.empty((T, geom.Hq, 128), dtype=torch.float16, device=dev)
+    else:
+        _need(out, torch.float16, "out")
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    row_max = torch.empty((geom.Hq, T), dtype=torch.float32, device=dev) if want_stats else None
+    row_sum = torch.empty((geom.Hq, T), dtype=torch.float32, device=dev) if want_stats else None
+    if workspace is None:
+        workspace = page_attn_workspace(geom, T, dev)
+    device = _same_device(q, k_pages=k_pages, v_pages=v_pages, q_start=q_start, ctx_len=ctx_len, table=table, out=out, workspace=workspace)
+    _launch(load_library().antkv_page_attn, "antkv_page_attn", device, geom._c, _p(q), q.stride(0) if T > 1 else 0,
+            q.stride(1) if geom.Hq > 1 else 0, T, _p(q_start), _p(ctx_len), _p(table), table.shape[1], _p(k_pages), _p(v_pages), n_pages,
+            page_size, float(scale), int(window), int(n_sink), _p(out), _p(row_max), _p(row_sum), _p(workspace), workspace.numel(), _stream(q))
+    return out, row_max, row_sum

@@ -28,6 +28,19 @@ int check_geom(const antkv_geom* gm, Geom& g)
 
 inline bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
+// n_pages pages of page_size tokens; every slot number fits 32 bits
+int check_pages(int64_t n_pages, int32_t page_size, Pages& pg)
+{
+    if (n_pages < 1 || page_size < 1) return ANTKV_EINVAL;
+    if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1)) != 0) return ANTKV_EUNSUPPORTED;
+    if (n_pages > 0x7fffffffLL / page_size) return ANTKV_EINVAL;
+    pg.n = n_pages;
+    pg.shift = __builtin_ctz((unsigned)page_size);
+    return ANTKV_OK;
+}
+// a block table of so many entries a row; positions stay below 2^30
+inline bool bad_table(int64_t table_cap, const Pages& pg) { return table_cap < 1 || table_cap > (1LL << 30) >> pg.shift; }
+
 struct SelPlan {
     size_t off_score, off_topk, total;
 };
@@ -274,6 +287,114 @@ int antkv_prefill_attn(const antkv_geom* geom, const void* q, const void* k, con
     const hipError_t e = launch_prefill_attn(g, (const half_t*)q, (const half_t*)k, (const half_t*)v, N, Nq, scale,
                                              (half_t*)out, row_max, row_sum, (hipStream_t)stream);
     return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+}
+
+int antkv_prefill_attn_window(const antkv_geom* geom, const void* q, const void* k, const void* v, int64_t N, int64_t Nq, float scale,
+                              int64_t window, int64_t n_sink, void* out, float* row_max, float* row_sum, void* stream)
+{
+    Geom g;
+    const int rc = check_geom(geom, g);
+    if (rc) return rc;
+    if (N <= 0 || Nq <= 0 || Nq > N || N > 1LL << 30 || window < 1 || n_sink < 0) return ANTKV_EINVAL;
+    if (Nq * g.G > 0x7fffffffLL || (Nq * g.G + 127) / 128 * g.B * g.Hkv > 0x7fffffffLL) return ANTKV_EINVAL;
+    if ((row_max == nullptr) != (row_sum == nullptr)) return ANTKV_EINVAL;
+    if (g.B == 0) return ANTKV_OK;
+    if (!q || !k || !v || !out) return ANTKV_EINVAL;
+    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(out, 16)) return ANTKV_EINVAL;
+    if (!(scale > 0.f)) return ANTKV_EINVAL;
+    const hipError_t e = launch_prefill_attn_window(g, (const half_t*)q, (const half_t*)k, (const half_t*)v, N, Nq, scale,
+                                                    (int)(window < N ? window : N), (int)(n_sink < N ? n_sink : N), (half_t*)out, row_max,
+                                                    row_sum, (hipStream_t)stream);
+    return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+}
+
+int antkv_page_map(int64_t R, const int32_t* held_len, const int32_t* new_len, int32_t* table, int64_t table_cap, int64_t n_pages,
+                   int32_t page_size, const int32_t* free_pages, int64_t n_free, const int32_t* free_at, int64_t T, int32_t* ctx_len,
+                   int32_t* q_start, int32_t* slot, int32_t* status, void* stream)
+{
+    Pages pg;
+    const int rc = check_pages(n_pages, page_size, pg);
+    if (rc) return rc;
+    if (R < 0 || bad_table(table_cap, pg) || n_free < 0 || n_free > 0x7fffffffLL || T < 0 || T > 0x7fffffffLL) return ANTKV_EINVAL;
+    if (R > kMapRequests) return ANTKV_EUNSUPPORTED;
+    if (!q_start || !status || status == free_at || (T > 0 && !slot) || (n_free > 0 && !free_pages)) return ANTKV_EINVAL;
+    if (R > 0 && (!held_len || !new_len || !table || !ctx_len || ctx_len == held_len || ctx_len == new_len)) return ANTKV_EINVAL;
+    const hipError_t e = launch_page_map(pg, (int)R, held_len, new_len, table, table_cap, free_pages, n_free, free_at, T, ctx_len, q_start, slot,
+                                         status, (hipStream_t)stream);
+    return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+}
+
+int antkv_page_store(const antkv_geom* geom, const void* k, const void* v, int64_t xs_t, int64_t xs_h, int64_t T, const int32_t* slot,
+                     void* k_pages, void* v_pages, int64_t n_pages, int32_t page_size, void* stream)
+{
+    Geom g;
+    int rc = check_geom(geom, g);
+    if (rc) return rc;
+    Pages pg;
+    rc = check_pages(n_pages, page_size, pg);
+    if (rc) return rc;
+    if (T < 0 || T > 0x7fffffffLL || T * g.Hkv > 0x7fffffffLL) return ANTKV_EINVAL;
+    if (T == 0) return ANTKV_OK;
+    if (!k || !v || !slot || !k_pages || !v_pages || k_pages == v_pages) return ANTKV_EINVAL;
+    if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16)) return ANTKV_EINVAL;
+    if ((xs_t & 7) || (xs_h & 7) || xs_t < 0 || xs_h < 0) return ANTKV_EINVAL;
+    const hipError_t e = launch_page_store(g.Hkv, pg, (const half_t*)k, (const half_t*)v, xs_t, xs_h, T, slot, (half_t*)k_pages, (half_t*)v_pages,
+                                           (hipStream_t)stream);
+    return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+}
+
+int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_pages, int64_t n_pages, int32_t page_size,
+                    const int32_t* table, int64_t table_cap, const int32_t* ctx_len, int64_t first, int64_t N, void* k, void* v,
+                    int64_t xs_b, int64_t xs_h, int64_t xs_t, void* stream)
+{
+    Geom g;
+    int rc = check_geom(geom, g);
+    if (rc) return rc;
+    Pages pg;
+    rc = check_pages(n_pages, page_size, pg);
+    if (rc) return rc;
+    if (bad_table(table_cap, pg) || first < 0 || N < 0 || first > table_cap << pg.shift || N > (table_cap << pg.shift) - first) return ANTKV_EINVAL;
+    if (N == 0 || g.B == 0) return ANTKV_OK;
+    if (!k_pages || !v_pages || !table || !k || !v || k == v) return ANTKV_EINVAL;
+    if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16)) return ANTKV_EINVAL;
+    if (xs_t < kD || (xs_b & 7) || (xs_h & 7) || (xs_t & 7) || xs_b < 0 || xs_h < 0) return ANTKV_EINVAL;
+    const hipError_t e = launch_page_load(g.B, g.Hkv, pg, (const half_t*)k_pages, (const half_t*)v_pages, table, table_cap, ctx_len, first, N,
+                                          (half_t*)k, (half_t*)v, xs_b, xs_h, xs_t, (hipStream_t)stream);
+    return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+}
+
+size_t antkv_page_attn_workspace(const antkv_geom* geom, int64_t T)
+{
+    Geom g;
+    if (check_geom(geom, g) || T < 1 || T > 0x7fffffffLL / g.Hq || g.B == 0) return 0;
+    return page_attn_workspace_bytes(g, T);
+}
+
+int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t qs_h, int64_t T, const int32_t* q_start,
+                    const int32_t* ctx_len, const int32_t* table, int64_t table_cap, const void* k_pages, const void* v_pages,
+                    int64_t n_pages, int32_t page_size, float scale, int64_t window, int64_t n_sink, void* out, float* row_max,
+                    float* row_sum, void* workspace, size_t workspace_bytes, void* stream)
+{
+    Geom g;
+    int rc = check_geom(geom, g);
+    if (rc) return rc;
+    Pages pg;
+    rc = check_pages(n_pages, page_size, pg);
+    if (rc) return rc;
+    if (T < 0 || T > 0x7fffffffLL / g.Hq || bad_table(table_cap, pg) || window < 0 || window > 1LL << 30 || n_sink < 0) return ANTKV_EINVAL;
+    if (n_pages * g.Hkv > 0x7fffffffLL / (page_size / 16)) return ANTKV_EINVAL;
+    if ((row_max == nullptr) != (row_sum == nullptr) || !(scale > 0.f)) return ANTKV_EINVAL;
+    if (T == 0 || g.B == 0) return ANTKV_OK;
+    if (!q || !q_start || !ctx_len || !table || !k_pages || !v_pages || !out) return ANTKV_EINVAL;
+    if (misaligned(q, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16) || misaligned(out, 16)) return ANTKV_EINVAL;
+    if ((qs_t & 7) || (qs_h & 7) || qs_t < 0 || qs_h < 0) return ANTKV_EINVAL;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < page_attn_workspace_bytes(g, T)) return ANTKV_EWORKSPACE;
+    PageAttnArgs a;
+    a.q = (const half_t*)q; a.qs_t = qs_t; a.qs_h = qs_h; a.T = T; a.q_start = q_start; a.ctx_len = ctx_len; a.table = table;
+    a.table_cap = table_cap; a.k_pages = (const half_t*)k_pages; a.v_pages = (const half_t*)v_pages; a.scale = scale;
+    a.window = (int)window; a.n_sink = (int)(n_sink < 1LL << 30 ? n_sink : 1LL << 30);
+    a.out = (half_t*)out; a.row_max = row_max; a.row_sum = row_sum;
+    return launch_page_attn(g, pg, a, workspace, (hipStream_t)stream) == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
 }
 
 int antkv_anchor_select(const antkv_geom* geom, const void* q, const void* k_fp16, int64_t N, int64_t Nq, float scale,

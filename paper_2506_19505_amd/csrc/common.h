@@ -154,6 +154,36 @@ hipError_t launch_anchor_score(const Geom& g, const half_t* q, const half_t* k, 
                                float scale, const float* row_max, const float* row_sum,
                                float* ans_k, float* ans_v, void* ws, bool room, hipStream_t st);
 
+// ---- a cache in pages: [n][Hkv][1 << shift tokens][D] fp16, one array for K and one for V ------------------------------------
+struct Pages {
+    int64_t n;
+    int shift;
+};
+constexpr int kMapRequests = 8192;                                  // requests of a step, at most (two prefix sums in LDS)
+hipError_t launch_page_map(const Pages& pg, int R, const int32_t* held, const int32_t* fresh, int32_t* table, int64_t table_cap,
+                           const int32_t* free_pages, int64_t n_free, const int32_t* free_at, int64_t T_cap, int32_t* ctx_len,
+                           int32_t* q_start, int32_t* slot, int32_t* status, hipStream_t st);
+hipError_t launch_page_store(int Hkv, const Pages& pg, const half_t* k, const half_t* v, int64_t xs_t, int64_t xs_h, int64_t T,
+                             const int32_t* slot, half_t* k_pages, half_t* v_pages, hipStream_t st);
+hipError_t launch_page_load(int B, int Hkv, const Pages& pg, const half_t* k_pages, const half_t* v_pages, const int32_t* table,
+                            int64_t table_cap, const int32_t* ctx_len, int64_t first, int64_t N, half_t* k, half_t* v, int64_t xs_b,
+                            int64_t xs_h, int64_t xs_t, hipStream_t st);
+struct PageAttnArgs {
+    const half_t* q;
+    int64_t qs_t, qs_h, T;
+    const int32_t *q_start, *ctx_len, *table;
+    int64_t table_cap;
+    const half_t *k_pages, *v_pages;
+    float scale;
+    int window, n_sink;                                             // window 0: every earlier key is visible
+    half_t* out;
+    float *row_max, *row_sum;
+};
+size_t page_attn_workspace_bytes(const Geom& g, int64_t T);
+hipError_t launch_page_attn(const Geom& g, const Pages& pg, const PageAttnArgs& a, void* ws, hipStream_t st);
+hipError_t launch_prefill_attn_window(const Geom& g, const half_t* q, const half_t* k, const half_t* v, int64_t N, int64_t Nq, float scale,
+                                      int window, int n_sink, half_t* out, float* row_max, float* row_sum, hipStream_t st);
+
 struct DecodeArgs {
     const half_t* q;
     float scale;
