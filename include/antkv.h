@@ -338,7 +338,7 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
                     int64_t xs_b, int64_t xs_h, int64_t xs_t, void* stream);
 
 /*
- * Attention of a step's new tokens over the paged cache, in which their own K and V are stored already.  geom->B = R requests; rows
+ * Attention of a step's new tokens over the paged cache, in which their own K and V are stored already.  geom->B = R requests (8192 at most); rows
  * q_start[r] .. q_start[r + 1] - 1 of the packed batch are the LAST positions of request r's ctx_len[r] tokens: row q_start[r] + i stands
  * at position ctx_len[r] - n + i (n its number of rows) and sees keys j up to its own position; with window >= 1 only those
  * with j > position - window or j < n_sink (window 0: no limit, at most 2^30).  Any mix of requests with no, one or thousands of rows.

@@ -366,7 +366,7 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
 size_t antkv_page_attn_workspace(const antkv_geom* geom, int64_t T)
 {
     Geom g;
-    if (check_geom(geom, g) || T < 1 || T > 0x7fffffffLL / g.Hq || g.B == 0) return 0;
+    if (check_geom(geom, g) || g.B > kMapRequests || T < 1 || T > 0x7fffffffLL / g.Hq || g.B == 0) return 0;
     return page_attn_workspace_bytes(g, T);
 }
 
@@ -381,6 +381,7 @@ int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t
     Pages pg;
     rc = check_pages(n_pages, page_size, pg);
     if (rc) return rc;
+    if (g.B > kMapRequests) return ANTKV_EUNSUPPORTED;
     if (T < 0 || T > 0x7fffffffLL / g.Hq || bad_table(table_cap, pg) || window < 0 || window > 1LL << 30 || n_sink < 0) return ANTKV_EINVAL;
     if (n_pages * g.Hkv > 0x7fffffffLL / (page_size / 16)) return ANTKV_EINVAL;
     if ((row_max == nullptr) != (row_sum == nullptr) || !(scale > 0.f)) return ANTKV_EINVAL;

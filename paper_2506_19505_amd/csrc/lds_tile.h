@@ -11,6 +11,7 @@ typedef __attribute__((address_space(3))) unsigned char lds_byte;
 typedef __attribute__((address_space(3))) short4_t lds_short4;
 typedef __attribute__((address_space(3))) half8_t lds_half8;
 typedef __attribute__((address_space(3))) float4_t lds_float4;
+typedef __attribute__((address_space(3))) uint4_t lds_uint4;
 
 // Rows of a tile are 16 chunks of 16 bytes; chunk c of row r sits at place c ^ swz(r).  The 16-byte reads of 16 rows (an
 // operand with the rows on its first axis) and the 4 rows x 64 bytes of a transposed read then fall on 64 different banks.

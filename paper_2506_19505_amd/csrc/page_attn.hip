@@ -1,29 +1,17 @@
-// Attention of new tokens over a paged cache (one token to thousands a request, a ragged batch in one launch), and over a dense
-// prompt, both with an optional window: a query at position p sees keys j <= p with j > p - window or j < n_sink.
+// Attention of a step's new tokens over a paged cache: any mix of requests with one token and with thousands, in one launch of
+// workgroups that share the work (span_attn.h has the rows, the tiles and the arithmetic).
 //
-// Rows.  The query rows of a request and KV head are its tokens x the G heads of the group, heads fastest: 32 consecutive rows are
-// a wave's tile (32 / G tokens), NW such tiles a block, which one workgroup handles over a range of keys.  So one token of a
-// group of four is a tile of four rows (memory is what bounds it), and a long chunk fills 8 x 32 rows per key tile that is read.
+// Work.  A request's rows of a KV head (tokens x G) are blocks of 32 to a wave; a block costs its key tiles and a constant for coming
+// and going.  Laid end to end, the costs of all blocks are cut into equal shares, one for each of the workgroups that the chip holds at a
+// time (the KV heads on their own XCDs), wherever the cuts fall: the middle of a long context, or behind a few short
+// ones.  Every workgroup derives the same cuts from the requests' lengths.  A block that is cut leaves partial sums, which the
+// last of its workgroups to end adds up.  With many blocks (kBlocksEach to a workgroup) each is a workgroup of its own instead.
 //
-// Keys.  Tiles of 32 keys go from global memory straight into LDS (16 bytes per lane, no registers), four tiles of K and of V in
-// flight or in use, shared by the workgroup's waves.  The page of every 16 keys of the range is looked up once, into LDS.
-//   scores   S^T tile (keys on the MFMA row axis, queries on the column axis): lane (n, kh) owns query row n and 16 of the
-//            tile's 32 keys, so the running softmax is lane-local; the two half-waves of a row meet only when the
-//            reference moves and at the end.
-//   output   O^T += V^T P^T: the B operand is the lane's own 16 probabilities (fp16), the A operand comes out of the V tile
-//            through ds_read_b64_tr_b16.
-// Probabilities are exp2 against a per-row reference kLift below the largest score when it was set: it moves when a score comes
-// more than kPMax above it.  Rounded to fp16 they then keep 11 bits down to 2^-22 of the largest one and 2^-32 as a step, so that
-// many small weights beside a large one are not lost; their sum is taken before the rounding, in fp32.
-//
-// Tiles that every row of a wave sees whole go four at a time through a loop that works on three at once (softmax of t, scores of
-// t + 1, value product of t - 1).  Tiles that some row sees in part (the diagonal, the window's left edge, the end of the sinks,
-// the end of the context, a page that is not one) go one by one: scores are masked, and where the tile's V is not finite the
-// value product keeps hidden rows out of the sum (0 x inf) by counting what each query sees of them.
-//
-// Split.  Few rows over long contexts leave CUs idle: the key tiles of a block are cut into ranges of about the same
-// work over all requests (every workgroup derives the plan from the lengths), partial sums meet in a second kernel.
-#include "lds_tile.h"
+// Wide blocks, of more than 32 rows: the waves have 32 rows each and share the key tiles (wide_sums).
+// Narrow blocks (a token or a few of a request): there is one tile of rows, and memory is what bounds it.  Every wave streams key tiles
+// of its own through 16 KB of LDS, K of the next tile under the softmax of this one and V under the scores of the next, without a
+// barrier; the waves' sums meet in LDS.
+#include "span_attn.h"
 
 #include <type_traits>
 
@@ -31,65 +19,23 @@ namespace antkv {
 
 namespace {
 
-constexpr int kRing = 4;                                // tiles of K, and of V, in LDS
-constexpr int kRingBytes = 2 * kRing * kTileBytes;
-constexpr int kChunk = 1024;                            // key tiles whose pages are looked up at a time
-constexpr float kPMax = 15.f, kLift = 8.f;
-constexpr float kMasked = -INFINITY;                    // a score that takes no part
+using namespace span;
 
-struct Params {
-    const half_t *q, *k, *v;
-    half_t* out;
-    float *row_max, *row_sum;
-    int64_t qs_b, qs_t, qs_h, os_b, os_t, os_h, st_b, st_h;         // strides in elements: q, out, statistics (per token 1)
-    float c1;
-    int Hkv, G, gs;                                                 // gs = log2 G
-    int window, n_sink;
-    // dense
-    int N, Nq, q_blocks;
-    // paged
-    const int32_t *q_start, *ctx_len, *table;
-    int64_t table_cap, n_pages;
-    int T, R, shift, target;                                        // target: key ranges over all requests, per KV head
-    int4_t* plan;                                                   // [T]: ranges, rows of the request, its first partial row, the token's first row
-    float4_t* part_stat;                                            // [partial rows]: reference, sum, largest score
-    float* part_out;                                                // [partial rows][D]
-    int64_t part_rows;
+constexpr int kNarrow = 32;
+constexpr int kWindow = 64;                                         // requests that a wave looks at at a time
+constexpr int kWindows = kMapRequests / kWindow;
+constexpr int kBlocksEach = 4;
+constexpr int kWaves = 2048;                                        // that the chip holds at a time: two to a SIMD
+
+template <int NW>                                       // waves of a workgroup: 8 or 4
+struct Lds {
+    static constexpr int tiles = 0;                                 // narrow: a K and a V tile per wave; wide: the rings
+    static constexpr int place = NW * 2 * kTileBytes;               // [kTurn][2]: places of the turn's key tiles
+    static constexpr int stat = place + kTurn * 8;                  // [NW][kNarrow][4]: reference, sum, largest score
+    static constexpr int total = stat + NW * kNarrow * 16;
+    static_assert(kRingBytes <= place && (total + kWindows * 8 + 1024) * (8 / NW) <= 163840, "LDS of a CU");
 };
 
-__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }      // of a value that is the same in every lane
-__device__ __forceinline__ float max3f(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
-
-// Key tiles that rows at positions lo .. hi of a context see: tiles 0 .. sink_tiles - 1, then from sink_tiles + gap on.
-struct Span {
-    int keys;                                                       // positions below this one are seen, at most
-    int sink_tiles, gap, n;
-    __device__ __forceinline__ int tile(int u) const { return u < sink_tiles ? u : u + gap; }
-};
-__device__ __forceinline__ Span span_of(int lo, int hi, int limit, int window, int n_sink)
-{
-    Span s;
-    s.keys = hi + 1 < limit ? hi + 1 : limit;
-    if (s.keys < 0) s.keys = 0;
-    const int end = (int)(((uint32_t)s.keys + 31u) >> 5);
-    s.sink_tiles = 0;
-    s.gap = 0;
-    if (window > 0) {
-        int from = lo - window + 1;
-        from = from > 0 ? from >> 5 : 0;
-        if (from > end) from = end;
-        const int sinks = n_sink < s.keys ? n_sink : s.keys;
-        s.sink_tiles = (int)(((uint32_t)sinks + 31u) >> 5);
-        s.gap = from > s.sink_tiles ? from - s.sink_tiles : 0;
-    }
-    s.n = end - s.gap;
-    return s;
-}
-
-// One request: its tokens in the packed batch and where they stand.
-struct Request {
-    int t0, n, p0, limit;                                           // first token, tokens, position of the first, keys that exist
-};
 __device__ __forceinline__ Request request_of(const Params& p, int r)
 {
     const int64_t a = p.q_start[r], e = p.q_start[r + 1], ctx = p.ctx_len[r];
@@ -98,571 +44,606 @@ __device__ __forceinline__ Request request_of(const Params& p, int r)
     int64_t p0 = ctx - (e > a ? e - a : 0) + (t0 - a);
     if (p0 < -(1 << 30)) p0 = -(1 << 30);
     if (p0 > 0x7fffffffLL - T) p0 = 0x7fffffffLL - T;
-    Request q;
-    q.t0 = (int)t0;
-    q.n = (int)(t1 - t0);
-    q.p0 = (int)p0;
-    q.limit = (int)(ctx < 0 ? 0 : ctx < have ? ctx : have);
-    return q;
+    return {(int)t0, (int)(t1 - t0), (int)p0, (int)(ctx < 0 ? 0 : ctx < have ? ctx : have)};
 }
 
-// What a workgroup works on.
-struct Item {
-    Request rq;
-    int r, block, range, ranges, from, to;                          // key tiles from .. to - 1 of the block's span
-    int64_t part;                                                   // first partial row of the request
+// ---- the plan --------------------------------------------------------------------------------------------------------------------
+
+// Costs of a request's blocks, last one (the longest) first: a, a - step, a - 2 step, ..
+template <int NW>
+struct Cost {
+    static constexpr int kRows = 32 * NW;                           // of a block
+    int blocks, a, step;
+    __device__ __forceinline__ Cost(const Params& p, const Request& q)
+    {
+        const int rows = q.n << p.gs;
+        blocks = (rows + kRows - 1) / kRows;
+        a = step = 0;
+        if (blocks > 0) {
+            const int first = (blocks - 1) * (kRows >> p.gs);
+            a = span_of(q.p0 + first, q.p0 + q.n - 1, q.limit, p.window, p.n_sink).n + idle(rows);
+            // causal: each block sees as many tiles less as it has tokens / 32; not so in a window, or where the table ends early
+            if (p.window == 0 && q.p0 >= 0 && q.p0 + q.n <= q.limit) step = kRows / 32 >> p.gs;
+        }
+    }
+    // Key tiles' worth of coming and going: looking up pages, the first loads, partial sums.  64 requests of 1 .. 32768 keys, a token each,
+    // with 4, 14, 20, 28, 40: 247, 202, 192, 178, 179 us in workgroups of 8 waves, with 10, 20, 28: 187, 181, 180 in workgroups of 4
+    __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? 20 : 16; }
+    __device__ __forceinline__ int before(int k) const { return k * a - step * (k * (k - 1) / 2); }      // of blocks 0 .. k - 1
+    __device__ __forceinline__ int all() const { return before(blocks); }
+    __device__ __forceinline__ int block_at(int x) const            // the block in which x lies
+    {
+        int k;
+        if (blocks == 1) k = 0;
+        else if (step == 0) k = x / a;
+        else {
+            const float u = 2.f * a + step;
+            k = (int)((u - sqrtf(fmaxf(u * u - 8.f * step * (float)x, 0.f))) / (2.f * step));
+            k = k < 0 ? 0 : k < blocks ? k : blocks - 1;
+            while (k > 0 && before(k) > x) --k;
+            while (k + 1 < blocks && before(k + 1) <= x) ++k;
+        }
+        return k;
+    }
 };
 
-// ranges of a request: about `most` tiles each, at least so many that partial sums stay cheap beside them
-template <int NW>
-__device__ __forceinline__ int ranges_of(const Request& q, const Span& s, int gs, int most)
+// inclusive sums over the wave (register moves between lanes: within rows of 16, then across them)
+template <int kCtrl, int kMask>
+__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, kCtrl, kMask, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int x)
 {
-    const int rows = q.n << gs, wide = rows < 32 * NW ? rows : 32 * NW;
-    int least = wide >> 3;
-    least = least < 4 ? 4 : least;
-    const int len = most > least ? most : least;
-    const int n = (s.n + len - 1) / len;
-    return n < 1 ? 1 : n;
+    x += from_lane<0x111, 0xf>(x);
+    x += from_lane<0x112, 0xf>(x);
+    x += from_lane<0x114, 0xf>(x);
+    x += from_lane<0x118, 0xf>(x);
+    x += from_lane<0x142, 0xa>(x);
+    return x + from_lane<0x143, 0xc>(x);
 }
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
-// Work item of this workgroup out of the lengths of all requests; false if there is none.  Every workgroup makes the same plan.
+// Where a workgroup is in the laid-out blocks: 64 requests at a time, one to a lane.  All other members are the same in every lane.
 template <int NW>
-__device__ bool find_item(const Params& p, int group, Item& it)
-{
-    constexpr int kT = NW * 64;
-    __shared__ int64_t s_sum[2][NW];
-    __shared__ int s_item[4];
-    __shared__ int64_t s_part;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    auto look = [&](int r, Request& q, Span& s) {
-        q = request_of(p, r);
-        const int blocks = ((q.n << p.gs) + 32 * NW - 1) / (32 * NW);
-        const int first = blocks > 0 ? (blocks - 1) * (32 * NW >> p.gs) : 0;
-        s = span_of(q.p0 + first, q.p0 + q.n - 1, q.limit, p.window, p.n_sink);
-        return blocks;
-    };
-    int64_t work = 0;
-    for (int r = tid; r < p.R; r += kT) {
-        Request q;
-        Span s;
-        work += (int64_t)look(r, q, s) * s.n;
-    }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) work += __shfl_xor(work, off, 64);
-    if (lane == 0) s_sum[0][wave] = work;
-    if (tid == 0) s_item[0] = -1;
-    __syncthreads();
-    work = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) work += s_sum[0][w];
-    const int64_t each = (work + p.target - 1) / p.target;
-    const int most = (int)(each < 0x7fffffff ? each : 0x7fffffff);
-    __syncthreads();
-    int64_t run_g = 0, run_p = 0;
-    for (int base = 0; base < p.R; base += kT) {
-        const int r = base + tid;
-        Request q;
-        Span s;
-        int64_t groups = 0, part = 0;
-        int blocks = 0, ranges = 1;
-        if (r < p.R) {
-            blocks = look(r, q, s);
-            ranges = ranges_of<NW>(q, s, p.gs, most);
-            groups = (int64_t)blocks * ranges;
-            part = ranges > 1 ? (int64_t)ranges * p.Hkv * (q.n << p.gs) : 0;
-        }
-        int64_t a = groups, b = part;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int64_t u = __shfl_up(a, off, 64), v = __shfl_up(b, off, 64);
-            if (lane >= off) { a += u; b += v; }
-        }
-        if (lane == 63) { s_sum[0][wave] = a; s_sum[1][wave] = b; }
-        __syncthreads();
-        int64_t all_g = 0, all_p = 0;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            if (w < wave) { a += s_sum[0][w]; b += s_sum[1][w]; }
-            all_g += s_sum[0][w];
-            all_p += s_sum[1][w];
-        }
-        const int64_t g0 = run_g + a - groups;
-        if (groups > 0 && group >= g0 && group < g0 + groups) {     // one thread of the workgroup
-            const int at = (int)(group - g0);
-            s_item[0] = r;
-            s_item[1] = blocks - 1 - at / ranges;                   // longest first
-            s_item[2] = at % ranges;
-            s_item[3] = ranges;
-            s_part = run_p + b - part;
-        }
-        run_g += all_g;
-        run_p += all_p;
-        __syncthreads();
-        if (run_g > group) break;                                   // (the same for every thread)
-    }
-    if (s_item[0] < 0) return false;
-    it.r = scalar(s_item[0]);
-    it.block = scalar(s_item[1]);
-    it.range = scalar(s_item[2]);
-    it.ranges = scalar(s_item[3]);
-    it.part = (int64_t)(uint32_t)scalar((int)s_part) | (int64_t)scalar((int)(s_part >> 32)) << 32;
-    it.rq = request_of(p, it.r);
-    it.rq.t0 = scalar(it.rq.t0);
-    it.rq.n = scalar(it.rq.n);
-    it.rq.p0 = scalar(it.rq.p0);
-    it.rq.limit = scalar(it.rq.limit);
-    // a batch whose starts are not ascending can ask for more than the workspace holds: its ranges are not cut then
-    if (it.ranges > 1 && it.part + (int64_t)it.ranges * p.Hkv * (it.rq.n << p.gs) > p.part_rows) {
-        if (it.range > 0) return false;
-        it.ranges = 1;
-    }
-    return true;
-}
+struct Cursor {
+    Request q;                                                      // the lane's request
+    int upto;                                                       // and the costs up to its end, from the window's start on
+    int window, base;                                               // first request / 64, costs before it
+    bool unit;                                                      // every block costs 1
 
-template <int NW, bool kPaged>                          // waves of a workgroup: 8 or 4
-__global__ __launch_bounds__(NW * 64, 2) void span_attn_kernel(const Params p)
-{
-    extern __shared__ __attribute__((aligned(1024))) unsigned char s_kv[];    // K ring, V ring; paged: pages of the range
-    constexpr int kParts = 8 / NW;                                  // pieces of 1 KB of a tile that a wave moves
-    lds_byte* lds = (lds_byte*)s_kv;
-    int* s_page = (int*)(s_kv + kRingBytes);                        // [key tiles][2]: place of 16 keys in the pool, -1 if there is none
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);      // scalar, so that per-wave conditions are scalar branches
-    const int n = lane & 31, kh = lane >> 5;
-    Item it;
-    int g, b;
-    if (kPaged) {
-        g = blockIdx.x % p.Hkv;                                     // heads fastest: 8 heads, one per XCD
-        b = 0;
-        if (!find_item<NW>(p, blockIdx.x / p.Hkv, it)) return;
-    } else {
-        const int bgs = gridDim.x / p.q_blocks, bg = blockIdx.x % bgs;
-        b = bg / p.Hkv;
-        g = bg % p.Hkv;
-        it.rq = {0, p.Nq, p.N - p.Nq, p.N};
-        it.r = 0;
-        it.block = p.q_blocks - 1 - blockIdx.x / bgs;               // longest rows first
-        it.range = 0;
-        it.ranges = 1;
-        it.part = 0;
-    }
-    const Request rq = it.rq;
-    const int rows = rq.n << p.gs, row0 = it.block * 32 * NW;
-    const int last_row = (row0 + 32 * NW < rows ? row0 + 32 * NW : rows) - 1;        // of the workgroup
-    const Span span = span_of(rq.p0 + (row0 >> p.gs), rq.p0 + (last_row >> p.gs), rq.limit, p.window, p.n_sink);
+    __device__ __forceinline__ int cost(const Params& p, const Request& u) const
     {
-        // every block of the request is cut at the same tiles, those of its longest
-        const int first = ((rows - 1) / (32 * NW)) * (32 * NW >> p.gs);
-        const Span longest = span_of(rq.p0 + first, rq.p0 + rq.n - 1, rq.limit, p.window, p.n_sink);
-        const int len = (longest.n + it.ranges - 1) / it.ranges;
-        it.from = it.range * len < span.n ? it.range * len : span.n;
-        it.to = it.range == it.ranges - 1 ? span.n : it.from + len < span.n ? it.from + len : span.n;
+        const Cost<NW> c(p, u);
+        return unit ? c.blocks : c.all();
     }
-    // the wave's rows: positions, and the keys a lane's row sees
-    const int w_row = row0 + 32 * wave;
-    const bool active = w_row < rows;
-    const int w_last = w_row + 31 < rows ? w_row + 31 : rows - 1;
-    const int w_lo = rq.p0 + (w_row >> p.gs), w_hi = rq.p0 + (w_last >> p.gs);
-    const int row = w_row + n < rows ? w_row + n : rows - 1;        // (rows behind the last repeat it and are not written)
-    const int tok = row >> p.gs, h = (g << p.gs) + (row & (p.G - 1));
-    const int pos = rq.p0 + tok;
-    const int key_hi = pos < rq.limit ? pos : rq.limit - 1;         // visible: j <= key_hi and (j >= key_lo or j < n_sink)
-    const int key_lo = p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0;
-    const int w_all = w_lo < rq.limit ? w_lo : rq.limit - 1;        // last key up to which every row sees what its window holds
-    // the keys of a tile that the lane's row sees, one bit each, from bit 0 on those of the half-wave: key 8 a + 4 kh + c at 8 a + c
-    auto below = [](int x) { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1u; };      // bits 0 .. x - 1
-    auto seen_of = [&](int tile, uint32_t bits) {
-        const int at = tile * 32;
-        const uint32_t w = below(key_hi + 1 - at) & (~below(key_lo - at) | below(p.n_sink - at));
-        return (w & ~((bits & 1 ? 0xffffu : 0u) | (bits & 2 ? 0xffff0000u : 0u))) >> (4 * kh);
-    };
-    auto bit_of = [](int r) { return 1u << (8 * (r >> 2) + (r & 3)); };                   // of accumulator register r
-    auto sees_all = [&](int tile) {                                 // every row of the wave sees every key of the tile
-        if (!active || tile * 32 + 31 > w_all) return false;
-        return p.window == 0 || tile * 32 > w_hi - p.window || tile * 32 + 31 < p.n_sink;
-    };
+    __device__ __forceinline__ void look(const Params& p)
+    {
+        const int r = window * kWindow + (threadIdx.x & 63);
+        q = r < p.R ? request_of(p, r) : Request{0, 0, 0, 0};
+        upto = wave_scan(cost(p, q));
+    }
+};
 
-    // staging: a wave moves kParts x 4 rows of a tile, a lane the chunk that belongs at its place of the 1 KB; rows behind the
-    // last key that the workgroup sees repeat it
+// ---- narrow blocks ---------------------------------------------------------------------------------------------------------------
+
+// Sums of up to 32 rows over the wave's share of the piece's key tiles: every NWth.
+template <int NW>
+__device__ __forceinline__ void narrow_sums(Sums& sums, const Params& p, const Piece& x, const Span& span, unsigned char* s_tiles, int* s_place)
+{
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, kh = lane >> 5, wave = scalar(tid >> 6);
+    const uint32_t k_at = (uint32_t)(uintptr_t)(lds_byte*)s_tiles + wave * (2 * kTileBytes), v_at = k_at + kTileBytes;
+    const Request rq = x.rq;
+    const int rows = rq.n << p.gs, row = n < rows ? n : rows - 1;
+    const int hi = rq.p0 + rq.n - 1, all = rq.p0 < rq.limit ? rq.p0 : rq.limit - 1;
+    const Sight sight(p, rq.p0 + (row >> p.gs), rq.limit);
     const int last_tile = (span.keys - 1) >> 5, last_key = (span.keys - 1) & 31;
-    uint32_t soff[kParts], soff_last[kParts];
+    // staging: 1 KB, four rows, per load; rows behind the last key repeat it
+    const int l4 = lane >> 4;
+    uint32_t soff[4];
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-        const int part = wave * kParts + i, r4 = 4 * part, r4l = r4 < (last_key & ~3) ? r4 : last_key & ~3;
-        const uint32_t chunk = ((lane & 15) ^ swz(r4 + (lane >> 4))) << 4;
-        const int in = lane >> 4, inl = in < last_key - r4l ? in : last_key - r4l;
-        soff[i] = ((kPaged ? r4 & 15 : r4) + in) * 256 + chunk;
-        soff_last[i] = ((kPaged ? r4l & 15 : r4l) + inl) * 256 + chunk;
-    }
-    const int half = wave * kParts * 4 >> 4;                        // which 16 keys of a tile this wave moves
-    const unsigned char* kbase = (const unsigned char*)(kPaged ? p.k : p.k + (int64_t)(b * p.Hkv + g) * p.N * kD);
-    const unsigned char* vbase = (const unsigned char*)(kPaged ? p.v : p.v + (int64_t)(b * p.Hkv + g) * p.N * kD);
-    const uint32_t to0 = (uint32_t)(uintptr_t)lds + wave * (kParts * 1024);
-    auto stage_at = [&](const unsigned char* base, int64_t off, bool last, uint32_t slot) {
+    for (int j = 0; j < 4; ++j) soff[j] = (4 * j + l4) * 256 + (((lane & 15) ^ swz(4 * j + l4)) << 4);
+    auto stage = [&](const half_t* pool, int a, int c, bool last, uint32_t to) __attribute__((always_inline)) {
+        const unsigned char* base[2] = {(const unsigned char*)pool + (int64_t)(a > 0 ? a : 0) * (16 * kD * 2), (const unsigned char*)pool + (int64_t)(c > 0 ? c : 0) * (16 * kD * 2)};
 #pragma unroll
-        for (int i = 0; i < kParts; ++i) load_to_lds16(base + off, last ? soff_last[i] : soff[i], to0 + slot * kTileBytes + 1024 * i);
-    };
-    // operand addresses inside a tile: K row n, channels 16 s + 8 kh .. + 7; V transposed: inside a 16-lane block, lane
-    // 4 e + c reads key row e of the lane's four, channels 4 c .. 4 c + 3 of 16; blocks 0/1 cover the two channel halves
-    // of a 32-channel group, blocks 2/3 the same for the other key half
-    uint32_t k_at[8], v_at[4][2];
-#pragma unroll
-    for (int s = 0; s < 8; ++s) { k_at[s] = tile_at(n, s, kh); pin(k_at[s]); }
-    {
-        const int e = (lane & 15) >> 2, c = lane & 3, blk = (lane >> 4) & 1;
-#pragma unroll
-        for (int cg = 0; cg < 4; ++cg)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int r = 8 * j + 4 * kh + e;
-                v_at[cg][j] = kRing * kTileBytes + r * 256 + (((4 * cg + 2 * blk + (c >> 1)) ^ swz(r)) << 4) + 8 * (c & 1);
-                pin(v_at[cg][j]);
+        for (int j = 0; j < 8; ++j) {
+            uint32_t off = soff[j & 3];
+            if (last) {
+                const int at = 4 * j + l4;
+                off = ((at < last_key ? at : last_key) & 15) * 256 + (off & 255);
             }
-    }
+            load_to_lds16(base[j >> 2], off, to + 1024 * j);
+        }
+    };
+    const Operands at(k_at, v_at, lane);
     half8_t tq[8];
-    {
-        const half_t* qp = p.q + b * p.qs_b + (int64_t)(rq.t0 + tok) * p.qs_t + h * p.qs_h + 8 * kh;
-#pragma unroll
-        for (int s = 0; s < 8; ++s) tq[s] = *(const half8_t*)(qp + 16 * s);
-#pragma unroll
-        for (int s = 0; s < 8; ++s) pin(tq[s]);
-    }
-
-    float16_t o[4], sc[2];
-    half8_t pr[2][2];
-#pragma unroll
-    for (int cg = 0; cg < 4; ++cg)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[cg][r] = 0.f;
-    float m_ref = kNegBig, s_max = kMasked, l_run = 0.f;            // reference (log2 units), largest raw score, sum
-    auto k_op = [&](int s, int slot) { return *(lds_half8*)(lds + k_at[s] + slot * kTileBytes); };
-    auto v_op = [&](int i, int slot) {                              // i = 4 * (16-key half) + channel group
-        const lds_byte* at = lds + slot * kTileBytes + (i >> 2) * 16 * 256;
-        const half4_t a = __builtin_bit_cast(half4_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(at + v_at[i & 3][0])));
-        const half4_t c = __builtin_bit_cast(half4_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(at + v_at[i & 3][1])));
-        return half8_t{a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
-    };
-    // accumulator register r of a score tile, and k-slot r & 7 of 16-key half r >> 3, is key 8 (r >> 2) + 4 kh + (r & 3)
-
-    for (int ua = it.from; ua < it.to; ua += kChunk) {
-        const int m = it.to - ua < kChunk ? it.to - ua : kChunk;    // tiles of this turn; i counts them
-        auto tile_of = [&](int i) { return span.tile(ua + (i < m ? i : m - 1)); };
-        // A page's place is counted in 16 keys of one head.  bad: two bits a tile (its 16-key halves), tile i at the bottom
-        uint32_t bad = 0;
-        int page_ahead[2] = {0, 0};                                 // of the tile that the next step asks for
-        int pv[2] = {0, 0}, pk = 0;                                 // places of tiles i + 2, i + 3 (V) and i + 4 (K)
-        __syncthreads();                                            // the turn before has been read
-        if (kPaged) {
-            const int32_t* row_of = p.table + (int64_t)it.r * p.table_cap;
-            for (int x = tid; x < 2 * m; x += NW * 64) {
-                int at = span.tile(ua + (x >> 1)) * 32 + 16 * (x & 1);
-                if (at > ((span.keys - 1) & ~15)) at = (span.keys - 1) & ~15;
-                const int64_t page = row_of[at >> p.shift];
-                s_page[x] = page >= 0 && page < p.n_pages
-                                ? (int)(((page * p.Hkv + g) << (p.shift - 4)) + ((at & ((1 << p.shift) - 1)) >> 4)) : -1;
-            }
-            __syncthreads();
+    load_query(tq, p, x, row, lane);
+    for (int ua = x.from; ua < x.to; ua += kTurn) {
+        const int m = x.to - ua < kTurn ? x.to - ua : kTurn;
+        const int32_t* row_of = p.table + (int64_t)x.r * p.table_cap;
+        if (ua > x.from) __syncthreads();                           // the turn before has been read
+        for (int k = tid; k < 2 * m; k += NW * 64) {
+            int key = span.tile(ua + (k >> 1)) * 32 + 16 * (k & 1);
+            if (key > ((span.keys - 1) & ~15)) key = (span.keys - 1) & ~15;
+            s_place[k] = place_of(p, row_of, x.g, key);
         }
-        auto pages_of = [&](int i, int& a, int& c) {
-            const int x = i < m ? i : m - 1;
-            a = s_page[2 * x];
-            c = s_page[2 * x + 1];
-        };
-        auto offset_of = [&](int i, int place) -> int64_t {
-            if (kPaged) return (int64_t)(place > 0 ? place : 0) * (16 * kD * 2);
-            return (int64_t)tile_of(i) * kTileBytes;
-        };
-        auto place_of = [&](int i) { return kPaged ? __builtin_amdgcn_readfirstlane(s_page[2 * (i < m ? i : m - 1) + half]) : 0; };
-        for (int i = 0; i < 4; ++i) stage_at(kbase, offset_of(i, place_of(i)), tile_of(i) == last_tile, i);
-        for (int i = 0; i < 2; ++i) stage_at(vbase, offset_of(i, place_of(i)), tile_of(i) == last_tile, kRing + i);
-        if (kPaged) {
-            for (int i = 0; i < 5; ++i) {
-                int a, c;
-                pages_of(i, a, c);
-                bad |= (uint32_t)((a < 0 ? 1 : 0) | (c < 0 ? 2 : 0)) << (2 * i);
-            }
-            bad = __builtin_amdgcn_readfirstlane(bad);
-            pv[0] = place_of(2);
-            pv[1] = place_of(3);
-            pk = place_of(4);
-            pages_of(5, page_ahead[0], page_ahead[1]);
-        }
-        // the V slot of "tile -1" is multiplied with zero probabilities: it has to be finite
-#pragma unroll
-        for (int i = 0; i < kParts; ++i) *(uint4_t*)(s_kv + (2 * kRing - 1) * kTileBytes + (i * NW * 64 + tid) * 16) = uint4_t{0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) pr[1][i][j] = (half_t)0.f;
         wait_all_loads();
         __syncthreads();
-
-        // stages for step i and brings the places one tile on
-        auto stage_ahead = [&](int i) __attribute__((always_inline)) {
-            stage_at(kbase, offset_of(i + 4, pk), tile_of(i + 4) == last_tile, i & 3);
-            stage_at(vbase, offset_of(i + 2, pv[0]), tile_of(i + 2) == last_tile, kRing + ((i + 2) & 3));
-            if (kPaged) {
-                const int a = __builtin_amdgcn_readfirstlane(page_ahead[0]), c = __builtin_amdgcn_readfirstlane(page_ahead[1]);
-                pv[0] = pv[1];
-                pv[1] = pk;
-                pk = half ? c : a;
-                bad = bad >> 2 | (uint32_t)((a < 0 ? 1 : 0) | (c < 0 ? 2 : 0)) << 8;          // now of tiles i + 1 .. i + 5
-                pages_of(i + 6, page_ahead[0], page_ahead[1]);
-            }
+        const int mine = (m - wave + NW - 1) / NW;                  // tiles wave, wave + NW, .. of the turn
+        if (mine <= 0) continue;
+        auto tile_of = [&](int i) { return span.tile(ua + wave + NW * i); };
+        auto places = [&](int i, int& a, int& c) {
+            const int k = 2 * (wave + NW * (i < mine ? i : mine - 1));
+            a = s_place[k];
+            c = s_place[k + 1];
         };
-        auto scores = [&](float16_t& s, int slot) __attribute__((always_inline)) {
+        int a, c, va, vc;                                           // places of the tile that K, and V, are asked for next
+        places(0, a, c);
+        va = a = scalar(a);
+        vc = c = scalar(c);
+        stage(p.k, a, c, tile_of(0) == last_tile, k_at);
+        stage(p.v, a, c, tile_of(0) == last_tile, v_at);
+        bool odd = false;                                           // some edge tile's V was not finite
+#pragma unroll 1
+        for (int i = 0; i < mine; ++i) {
+            const int tile = tile_of(i);
+            const bool more_last = tile_of(i + 1 < mine ? i + 1 : i) == last_tile;
+            const uint32_t bits = (a < 0 ? 1 : 0) | (c < 0 ? 2 : 0);
+            int na, nc;
+            places(i + 1, na, nc);
+            asm volatile("s_waitcnt vmcnt(8)" ::: "memory");         // K has landed
+            float16_t s;
+            half8_t op[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) op[j] = at.k_op(j, 0);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_op(j, slot), tq[j], s, 0, 0, 0);
-        };
-        // largest score and reference before the exponentials of a tile; true if it moves (o has to be rescaled by alpha)
-        auto open_tile = [&](float16_t& s, float& alpha) __attribute__((always_inline)) {
-            s_max = max3f(s_max, s[0], s[1]);
-#pragma unroll
-            for (int r = 2; r < 16; r += 2) s_max = max3f(s_max, s[r], s[r + 1]);
-            alpha = 1.f;
-            const bool moves = __any(fmaf(s_max, p.c1, -m_ref) > kPMax);
-            if (__builtin_expect(moves, 0)) {                       // the reference moves to the largest score so far
-                const float m_new = fmaf(fmaxf(s_max, __shfl_xor(s_max, 32, 64)), p.c1, -kLift);
-                if (m_new + kLift - m_ref > kPMax) {
-                    alpha = fast_exp2(m_ref - m_new);
-                    l_run *= alpha;
-                    m_ref = m_new;
-                }
-            }
-            return moves;
-        };
-        auto rescale = [&](float alpha) __attribute__((always_inline)) {
-#pragma unroll
-            for (int cg = 0; cg < 4; ++cg)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[cg][r] *= alpha;
-        };
-        // value product of a tile whose probabilities are pr[1].  edge: some key of it is hidden from some row (seen: the lane's word), and
-        // counts as nothing for that row whatever its V holds: V that is not finite is left out, and comes back as inf, -inf or
-        // NaN where a row sees it
-        auto product = [&](int slot, bool edge, uint32_t seen) __attribute__((always_inline)) {
-            uint32_t odd = 0;
-            if (edge) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint4_t x = __builtin_bit_cast(uint4_t, v_op(i, slot));
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) odd |= ((x[j] & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
-                }
-            }
-            if (__builtin_expect(__any(odd != 0), 0)) {
-#pragma unroll
-                for (int cg = 0; cg < 4; ++cg) {
-                    float16_t c;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) c[r] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint4_t x = __builtin_bit_cast(uint4_t, v_op(4 * i + cg, slot)), kind, sees;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {               // two values at a time; 1: inf, 64: -inf, 4096: NaN (sums of 32 keep apart)
-                            uint32_t all = 0, ones = 0;
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const uint32_t y = x[j] >> (16 * e) & 0xffffu;
-                                const uint32_t of = (y & 0x7fffu) < 0x7c00u ? 0u : (y & 0x7fffu) > 0x7c00u ? 0x6c00u : y >> 15 ? 0x5400u : 0x3c00u;
-                                all |= of << (16 * e);
-                                if (seen & bit_of(8 * i + 2 * j + e)) ones |= 0x3c00u << (16 * e);
-                                if (of) x[j] &= e ? 0x0000ffffu : 0xffff0000u;
-                            }
-                            kind[j] = all;
-                            sees[j] = ones;
-                        }
-                        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, kind), __builtin_bit_cast(half8_t, sees), c, 0, 0, 0);
-                        o[cg] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, x), pr[1][i], o[cg], 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int count = (int)c[r];
-                        o[cg][r] += (count & 63 ? INFINITY : 0.f) - (count >> 6 & 63 ? INFINITY : 0.f) + (count >> 12 ? NAN : 0.f);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_op(i, slot), pr[1][i >> 2], o[i & 3], 0, 0, 0);
-            }
-        };
-
-        bool was_edge = false;                                      // some row does not see some key of tile i - 1
-        uint32_t seen = 0;                                          // its keys that the lane's row sees, where that is so
-        if (active) scores(sc[0], 0);
-        __syncthreads();                                            // step 0 stages over the tile that has just been read
-        int i = 0;
-        if (!active)                                                // a wave without rows stages for the others
-            for (; i < m; ++i) {
-                stage_ahead(i);
-                landed_but<4 * kParts>();
-            }
-#pragma unroll 1
-        for (; i < m; ++i) {
-            const int tile = tile_of(i);
-            const uint32_t bits = bad & 3;
-            stage_ahead(i);
-            product((i + 3) & 3, was_edge, seen);
-            was_edge = bits != 0 || !sees_all(tile);
-            if (was_edge) {
-                seen = seen_of(tile, bits);
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (!(seen & bit_of(r))) sc[0][r] = kMasked;
-            }
+            for (int j = 0; j < 8; ++j) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(op[j], tq[j], s, 0, 0, 0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // and has been read
+            a = scalar(na);
+            c = scalar(nc);
+            stage(p.k, a, c, more_last, k_at);                       // (behind the last tile: once more, which keeps the counts)
+            const bool edge = bits != 0 || !sight.whole(tile, all, hi);
+            if (__builtin_expect(edge, 0)) mask(s, sight.of_tile(tile, bits, kh));
             float alpha;
-            if (open_tile(sc[0], alpha)) rescale(alpha);
+            if (sums.open(s, p.c1, alpha)) sums.rescale(alpha);
             float sum[2] = {0.f, 0.f};
+            half8_t pr[2];
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float e = fast_exp2(fmaf(sc[0][r], p.c1, -m_ref));
+                const float e = fast_exp2(fmaf(s[r], p.c1, -sums.m_ref));
                 sum[r & 1] += e;
-                pr[1][r >> 3][r & 7] = (half_t)e;
+                pr[r >> 3][r & 7] = (half_t)e;
             }
-            l_run += sum[0] + sum[1];
-            scores(sc[0], (i + 1) & 3);
-            __builtin_amdgcn_sched_barrier(0);                      // (K and V have been read before another wave stages over them)
-            landed_but<4 * kParts>();
-        }
-        if (active) product((m + 3) & 3, was_edge, seen);
-        wait_all_loads();                                           // nothing may land in LDS after the turn, or the workgroup's end
-    }
-
-    const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-    s_max = fmaxf(s_max, __shfl_xor(s_max, 32, 64));
-    if (it.ranges > 1) {
-        if (active && w_row + n < rows) {
-            const int64_t at = it.part + ((int64_t)it.range * p.Hkv + g) * rows + row;
-            float* op = p.part_out + at * kD + 4 * kh;
-            if (l_tot != 0.f)                                       // (also where it is NaN)
+            sums.l += sum[0] + sum[1];
+            asm volatile("s_waitcnt vmcnt(8)" ::: "memory");         // V has landed
+            if (__builtin_expect(edge, 0)) {                        // hidden or not, what is not finite waits until the turn is over
 #pragma unroll
-                for (int cg = 0; cg < 4; ++cg)
+                for (int j = 0; j < 8; ++j) {
+                    lds_uint4* to = (lds_uint4*)(uintptr_t)(v_at + 1024 * j + lane * 16);
+                    uint4_t two = *to;
+                    uint32_t any = 0;
 #pragma unroll
-                    for (int qd = 0; qd < 4; ++qd)
-                        *(float4_t*)(op + 32 * cg + 8 * qd) = float4_t{o[cg][4 * qd], o[cg][4 * qd + 1], o[cg][4 * qd + 2], o[cg][4 * qd + 3]};
-            if (kh == 0) p.part_stat[at] = float4_t{m_ref, l_tot, s_max, 0.f};
-        }
-    } else if (active && w_row + n < rows) {
-        const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;         // a row that sees nothing is zero
-        half_t* op = p.out + b * p.os_b + (int64_t)(rq.t0 + tok) * p.os_t + h * p.os_h + 4 * kh;
-#pragma unroll
-        for (int cg = 0; cg < 4; ++cg)
-#pragma unroll
-            for (int qd = 0; qd < 4; ++qd) {                        // accumulator rows 8 qd + 4 kh + e = channels of group cg
-                half4_t w;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = (half_t)(o[cg][4 * qd + e] * inv);
-                *(half4_t*)(op + 32 * cg + 8 * qd) = w;
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t is = not_finite(two[e]);
+                        two[e] = without(two[e], is);
+                        any |= is;
+                    }
+                    if (any) *to = two;
+                    odd = odd || __any(any != 0);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
-        if (kh == 0 && p.row_max) {
-            const int64_t at = b * p.st_b + h * p.st_h + rq.t0 + tok;
-            p.row_max[at] = s_max * p.c1 * (1.f / kLog2e);
-            p.row_sum[at] = l_tot == 0.f ? 0.f : l_tot * fast_exp2(fmaf(-s_max, p.c1, m_ref));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) op[j] = at.v_op(j, 0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums.o[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op[j], pr[j >> 2], sums.o[j & 3], 0, 0, 0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            va = a;
+            vc = c;
+            stage(p.v, va, vc, more_last, v_at);
         }
+        if (__builtin_expect(odd, 0))
+            for (int i = 0; i < mine; ++i) {
+                places(i, a, c);
+                a = scalar(a);
+                c = scalar(c);
+                const uint32_t bits = (a < 0 ? 1 : 0) | (c < 0 ? 2 : 0);
+                if (bits == 0 && sight.whole(tile_of(i), all, hi)) continue;
+                wait_all_loads();
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                stage(p.v, a, c, tile_of(i) == last_tile, v_at);
+                wait_all_loads();
+                add_odd(sums, at, 0, sight.of_tile(tile_of(i), bits, kh));
+            }
+        wait_all_loads();                                           // nothing may land in LDS after the turn
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    if (kPaged && g == 0 && it.range == 0)                          // for the second kernel
-        for (int x = (row0 >> p.gs) + tid; x <= last_row >> p.gs; x += NW * 64)
-            p.plan[rq.t0 + x] = int4_t{it.ranges, rows, (int)(it.part & 0x7fffffff), x << p.gs};
+    sums.join_halves();
 }
 
-// Adds the partial sums of a row: a wave per row, two channels to a lane.
-constexpr int kMergeThreads = 256;
+// ---- partial sums ----------------------------------------------------------------------------------------------------------------
 
-__global__ __launch_bounds__(kMergeThreads) void merge_kernel(const Params p, int n_rows)
+// 8 bytes, past the caches of the die that wrote them: the workgroup that merges may sit on another
+__device__ __forceinline__ float2_t load_part(const float* x)
 {
-    const int lane = threadIdx.x & 63, Hq = p.Hkv << p.gs;
-    const int at = blockIdx.x * (kMergeThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (at >= n_rows) return;
-    const int t = at / Hq, h = at - t * Hq, g = h >> p.gs;
-    const int4_t plan = p.plan[t];
-    if (t < p.q_start[0] || t >= p.q_start[p.R]) return;            // a token that no request has
-    const int S = plan[0], rows = plan[1], row = plan[3] + (h & (p.G - 1));
-    const int64_t first = plan[2], stride = (int64_t)p.Hkv * rows;
-    if (S < 2 || S > p.part_rows || rows < 1 || row < 0 || row >= rows || first + S * stride > p.part_rows) return;
-    const float4_t* stat = p.part_stat + first + (int64_t)g * rows + row;
-    const float* part = p.part_out + (first + (int64_t)g * rows + row) * kD + 2 * lane;
-    float m = kNegBig, s_max = kMasked;
-    for (int s = lane; s < S; s += 64) {
-        const float4_t x = stat[s * stride];
-        if (x[1] != 0.f) m = fmaxf(m, x[0]);
-        s_max = fmaxf(s_max, x[2]);
+    return __builtin_bit_cast(float2_t, __hip_atomic_load((const unsigned long long*)x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+__device__ __forceinline__ void store_part(float* x, float a, float b)
+{
+    __hip_atomic_store((unsigned long long*)x, __builtin_bit_cast(unsigned long long, float2_t{a, b}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The pieces of a block that is cut: shares first .. last.  A share has at most one piece that goes on from the share before (slot
+// 2 share) and one that begins a block and does not end it (slot 2 share + 1).
+struct Pieces {
+    int first, last, start;                                         // start: the share in which the block's cost begins
+    __device__ __forceinline__ int64_t slot(const Params& p, int share, int g) const { return (int64_t)(2 * share + (share == start ? 1 : 0)) * p.Hkv + g; }
+};
+
+// Each wave waits until its stores are acknowledged, the barrier collects the waves, then one thread arrives: the last arrival reads
+// partial sums that have all reached the level its loads read from.  It leaves the word as (tag, 0): a captured launch that is
+// replayed over other lengths, and so other numbers of pieces, finds no arrivals.
+__device__ __forceinline__ bool last_to_arrive(unsigned long long* word, uint64_t tag, int pieces, int* s_flag)
+{
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const bool last = (int)(__hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & kArrivalMask) + 1 == pieces;
+        if (last) __hip_atomic_store(word, (unsigned long long)tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *s_flag = last;
     }
-    m = wave_max(m);
-    s_max = wave_max(s_max);
-    float l = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int s0 = 0; s0 < S; s0 += 64) {
-        float w = 0.f;
+    __syncthreads();
+    return scalar(*s_flag) != 0;
+}
+
+// Adds the partial sums of a row of a narrow block: a wave, two channels to a lane.
+__device__ __forceinline__ void merge_row(const Params& p, const Pieces& pc, int row, int g, int64_t t, int h, int lane)
+{
+    const int S = pc.last - pc.first + 1;
+    auto at = [&](int s) { return pc.slot(p, pc.first + s, g) * p.rows_cap + row; };
+    constexpr int kBatch = 16;
+    float m = kNegBig, s_max = kMasked, l = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int s0 = 0; s0 < S; s0 += 64) {                            // lane: piece s0 + lane
+        float2_t x = {kNegBig, 0.f}, y = {kMasked, 0.f};
         if (s0 + lane < S) {
-            const float4_t x = stat[(s0 + lane) * stride];
-            if (x[1] != 0.f) {
-                w = fast_exp2(x[0] - m);
-                l += x[1] * w;
-            }
+            const float* stat = p.part_stat + 4 * at(s0 + lane);
+            x = load_part(stat);
+            y = load_part(stat + 2);
         }
         const int most = S - s0 < 64 ? S - s0 : 64;
-        for (int s1 = 0; s1 < most; s1 += 8) {
-            float a[8], c[8];
-            float ws[8];
+        float2_t v[kBatch];
+        auto fetch = [&](int s1) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                ws[j] = s1 + j < most ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (s1 + j) & 63)) : 0.f;
-                a[j] = c[j] = 0.f;
-                if (ws[j] != 0.f) {                                 // (a range that nothing is seen of has written no sums)
-                    const float* x = part + (s0 + s1 + j) * stride * kD;
-                    a[j] = x[0];
-                    c[j] = x[1];
-                }
+            for (int j = 0; j < kBatch; ++j) v[j] = load_part(p.part_out + at(s0 + (s1 + j < most ? s1 + j : most - 1)) * kD + 2 * lane);
+        };
+        fetch(0);
+        const bool some = x[1] != 0.f;                              // (also where it is NaN)
+        s_max = fmaxf(s_max, wave_max(y[0]));
+        const float m_new = fmaxf(m, wave_max(some ? x[0] : kNegBig)), back = fast_exp2(m - m_new);
+        const float w = some ? fast_exp2(x[0] - m_new) : 0.f;
+        m = m_new;
+        l = l * back + wave_sum(some ? x[1] * w : 0.f);
+        o0 *= back;
+        o1 *= back;
+        for (int s1 = 0; s1 < most; s1 += kBatch) {
+            if (s1 > 0) fetch(s1);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const float ws = s1 + j < most ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (s1 + j) & 63)) : 0.f;
+                o0 = fmaf(v[j][0], ws, o0);
+                o1 = fmaf(v[j][1], ws, o1);
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) { o0 = fmaf(a[j], ws[j], o0); o1 = fmaf(c[j], ws[j], o1); }
         }
     }
-    l = wave_sum(l);
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    half_t* op = p.out + (int64_t)t * p.os_t + h * p.os_h + 2 * lane;
-    *(half2_t*)op = half2_t{(half_t)(o0 * inv), (half_t)(o1 * inv)};
+    *(half2_t*)(p.out + t * p.os_t + h * p.os_h + 2 * lane) = half2_t{(half_t)(o0 * inv), (half_t)(o1 * inv)};
     if (lane == 0 && p.row_max) {
         p.row_max[h * p.st_h + t] = s_max * p.c1 * (1.f / kLog2e);
         p.row_sum[h * p.st_h + t] = l == 0.f ? 0.f : l * fast_exp2(fmaf(-s_max, p.c1, m));
     }
 }
 
-template <int NW, bool kPaged>
-hipError_t launch_t(const Params& p, int64_t grid, hipStream_t st)
+// Wide blocks leave their registers as they are, 64 lanes x 16 bytes at a time.
+__device__ __forceinline__ float* wide_part(const Params& p, int64_t slot, int wave, int i, int lane)
 {
-    constexpr size_t lds = kRingBytes + (kPaged ? 2 * kChunk * sizeof(int) : 0);
-    static OncePerDevice once;
-    const hipError_t e = allow_lds(once, (const void*)span_attn_kernel<NW, kPaged>, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((span_attn_kernel<NW, kPaged>), dim3((unsigned)grid), dim3(NW * 64), lds, st, p);
-    return hipGetLastError();
+    return p.part_out + slot * p.rows_cap * kD + ((wave * 16 + i) * 64 + lane) * 4;
+}
+__device__ __forceinline__ void store_wide(const Params& p, const Sums& x, int64_t slot, int wave, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float* to = wide_part(p, slot, wave, i, lane);
+        store_part(to, x.o[i >> 2][4 * (i & 3)], x.o[i >> 2][4 * (i & 3) + 1]);
+        store_part(to + 2, x.o[i >> 2][4 * (i & 3) + 2], x.o[i >> 2][4 * (i & 3) + 3]);
+    }
+    if (lane < 32) {
+        float* stat = p.part_stat + 4 * (slot * p.rows_cap + 32 * wave + lane);
+        store_part(stat, x.m_ref, x.l);
+        store_part(stat + 2, x.s_max, 0.f);
+    }
+}
+__device__ __forceinline__ void merge_wide(const Params& p, Sums& x, const Pieces& pc, int g, int wave, int lane)
+{
+    x.clear();
+    for (int s = pc.first; s <= pc.last; ++s) {                     // always in the order of the keys
+        const int64_t slot = pc.slot(p, s, g);
+        const float* stat = p.part_stat + 4 * (slot * p.rows_cap + 32 * wave + (lane & 31));
+        const float2_t u = load_part(stat), v = load_part(stat + 2);
+        float2_t o[32];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float* from = wide_part(p, slot, wave, i, lane);
+            o[2 * i] = load_part(from);
+            o[2 * i + 1] = load_part(from + 2);
+        }
+        const bool some = u[1] != 0.f;                              // (also where it is NaN)
+        const float m_new = some ? fmaxf(x.m_ref, u[0]) : x.m_ref, back = fast_exp2(x.m_ref - m_new), w = some ? fast_exp2(u[0] - m_new) : 0.f;
+        x.m_ref = m_new;
+        x.s_max = fmaxf(x.s_max, v[0]);
+        x.l = x.l * back + (some ? u[1] * w : 0.f);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x.o[i >> 2][4 * (i & 3) + e] = fmaf(o[2 * i + (e >> 1)][e & 1], w, x.o[i >> 2][4 * (i & 3) + e] * back);
+    }
 }
 
-int log2_of(int G) { return G == 4 ? 2 : G == 2 ? 1 : 0; }
+// ---- the kernel ------------------------------------------------------------------------------------------------------------------
+
+template <int NW>
+__global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
+{
+    constexpr int kThreads = NW * 64, kRows = 32 * NW;
+    using At = Lds<NW>;
+    __shared__ __attribute__((aligned(1024))) unsigned char s_all[At::total];
+    __shared__ int s_cost[kWindows], s_blocks[kWindows], s_odd, s_flag;
+    int* s_place = (int*)(s_all + At::place);
+    float4_t* s_stat = (float4_t*)(s_all + At::stat);
+    const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6);
+    const int share = blockIdx.x / p.Hkv, n_shares = gridDim.x / p.Hkv, g = blockIdx.x % p.Hkv;      // (heads fastest: 8 heads, one per XCD)
+
+    // the costs of all requests
+    Cursor<NW> cur;
+    cur.window = cur.base = 0;
+    cur.unit = false;
+    const int windows = (p.R + kWindow - 1) / kWindow;
+    int total = 0, blocks = 0, wide = 0;
+    float about = 0.f;                                              // the total, where it does not fit an int
+    {
+        auto tally = [&](int& cost, int& some, bool& any_wide, float& f) {
+            const Cost<NW> c(p, cur.q);
+            some = last_lane(wave_scan(c.blocks));
+            cost = last_lane(cur.upto);
+            any_wide = __any((cur.q.n << p.gs) > kNarrow);
+            f = wave_sum((float)c.blocks * (float)c.a);
+        };
+        if (windows == 1) {
+            bool any;
+            cur.look(p);
+            tally(total, blocks, any, about);
+            wide = any;
+        } else {
+            if (tid == 0) s_flag = 0;
+            __syncthreads();
+            for (int w = wave; w < windows; w += NW) {
+                int cost, some;
+                bool any;
+                float f;
+                cur.window = w;
+                cur.look(p);
+                tally(cost, some, any, f);
+                if (lane == 0) {
+                    s_cost[w] = f < 1e8f ? cost : -1;
+                    s_blocks[w] = some;
+                    if (any) s_flag = 1;
+                }
+            }
+            __syncthreads();
+            wide = scalar(s_flag);
+            for (int w = 0; w < windows; ++w) {
+                const int c = scalar(s_cost[w]);
+                total += c < 0 ? 0 : c;
+                blocks += scalar(s_blocks[w]);
+                about += c < 0 ? 1e9f : (float)c;
+            }
+            cur.window = -1;
+        }
+    }
+    total = scalar(total);
+    blocks = scalar(blocks);
+    // All of the plan is the same in every lane, and has to be so to the compiler too: values that come out of a shuffle are not, and a
+    // loop over pieces on such values would be run under a mask of lanes.
+    cur.unit = scalar(blocks * p.Hkv >= kBlocksEach * (kWaves / NW) || about >= 1e9f) != 0;
+    wide = scalar(wide);
+    int size = 1, x = share, end = blocks;                          // the share: costs x .. end - 1 (unit: blocks x, x + n_shares, ..)
+    if (!cur.unit) {
+        size = (total + p.shares - 1) / p.shares;
+        const int least = wide ? 48 : 12;
+        if (size < least) size = least;
+        x = share < p.shares ? share * size : total;
+        end = x + size < total ? x + size : total;
+    }
+    if (x >= end) return;
+    if (windows == 1) {
+        if (cur.unit) cur.look(p);
+    } else {                                                        // the window of requests in which the share begins
+        const int* sums = cur.unit ? s_blocks : s_cost;
+        int w = 0, before = 0;
+        for (int c = scalar(sums[0]); w + 1 < windows && x >= before + c; c = scalar(sums[w])) {
+            before += c;
+            ++w;
+        }
+        cur.window = w;
+        cur.base = before;
+        cur.look(p);
+    }
+
+    for (;;) {
+        // the request in which x lies, its block, the block's pieces
+        while (x >= cur.base + last_lane(cur.upto)) {
+            if (cur.window + 1 >= windows) return;
+            cur.base += last_lane(cur.upto);
+            ++cur.window;
+            cur.look(p);
+        }
+        const int l = __builtin_ctzll(__ballot(x < cur.base + cur.upto));
+        Piece pc;
+        pc.b = 0;
+        pc.g = g;
+        pc.r = cur.window * kWindow + l;
+        pc.rq = {__builtin_amdgcn_readlane(cur.q.t0, l), __builtin_amdgcn_readlane(cur.q.n, l), __builtin_amdgcn_readlane(cur.q.p0, l), __builtin_amdgcn_readlane(cur.q.limit, l)};
+        const Request rq = pc.rq;
+        const Cost<NW> cost(p, rq);
+        const int rows = rq.n << p.gs;
+        const int begin = cur.base + __builtin_amdgcn_readlane(cur.upto, l) - (cur.unit ? cost.blocks : cost.all());      // of the request
+        const int k = scalar(cur.unit ? x - begin : cost.block_at(x - begin));
+        const int c0 = begin + (cur.unit ? k : cost.before(k)), len = cur.unit ? 1 : cost.a - cost.step * k;              // of the block
+        pc.row0 = (cost.blocks - 1 - k) * kRows;
+        const bool narrow = rows <= kNarrow;
+        const int last_row = (pc.row0 + kRows < rows ? pc.row0 + kRows : rows) - 1;
+        const Span span = span_of(rq.p0 + (pc.row0 >> p.gs), rq.p0 + (last_row >> p.gs), rq.limit, p.window, p.n_sink);
+        pc.from = 0;
+        pc.to = span.n;
+        Pieces all = {share, share, share};
+        bool some = true;                                           // the piece has tiles, or is the only one
+        if (!cur.unit) {
+            // cost offset -> tile: what lies behind the idle part, cut at every fourth (wide blocks are worked on four at a time)
+            const int idle = Cost<NW>::idle(rows), round = 4;
+            auto tile_at = [&](int off) { const int t = off - idle; return t <= 0 ? 0 : off >= len ? span.n : t / round * round < span.n ? t / round * round : span.n; };
+            all.start = c0 >= share * size ? share : c0 / size;
+            all.last = c0 + len <= (share + 1) * size ? share : (c0 + len - 1) / size;
+            all.first = (c0 + idle + round + size - 1) / size - 1;  // the first with a tile
+            if (all.first < all.start) all.first = all.start;
+            if (all.first > all.last) all.first = all.last;
+            some = share >= all.first;
+            pc.from = share == all.first ? 0 : tile_at(share * size - c0);
+            pc.to = share == all.last ? span.n : tile_at((share + 1) * size - c0);
+        }
+        if (some) {
+            const int pieces = all.last - all.first + 1;
+            unsigned long long* word = p.done + (int64_t)all.last * p.Hkv + g;
+            unsigned long long seen = 0;
+            if (pieces > 1 && tid == 0) seen = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            Sums sums;
+            sums.clear();
+            // An arrival word that another launch, or anything else, has left is replaced by (tag, 0) by whoever gets there first.
+            auto claim = [&]() {
+                if (pieces > 1 && tid == 0 && arrivals_are_stale(seen, p.tag, 1u << kArrivalBits))
+                    __hip_atomic_compare_exchange_strong(word, &seen, (unsigned long long)p.tag, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            };
+            const int64_t slot = all.slot(p, share, g);
+            if (narrow) {
+                narrow_sums<NW>(sums, p, pc, span, s_all + At::tiles, s_place);
+                claim();
+                // the waves' sums meet: rows of 32 x 16 bytes per wave, turned by the row (banks)
+                const int n = lane & 31, kh = lane >> 5;
+                float4_t* s_sum = (float4_t*)(s_all + At::tiles);
+                if (n < rows) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int c4 = 8 * (i >> 2) + 2 * (i & 3) + kh;
+                        s_sum[(wave * kNarrow + n) * 32 + ((c4 + n) & 31)] =
+                            float4_t{sums.o[i >> 2][4 * (i & 3)], sums.o[i >> 2][4 * (i & 3) + 1], sums.o[i >> 2][4 * (i & 3) + 2], sums.o[i >> 2][4 * (i & 3) + 3]};
+                    }
+                    if (kh == 0) s_stat[wave * kNarrow + n] = float4_t{sums.m_ref, sums.l, sums.s_max, 0.f};
+                }
+                __syncthreads();
+                for (int u = tid; u < rows * 32; u += kThreads) {
+                    const int row = u >> 5, c4 = u & 31, t = rq.t0 + (row >> p.gs), h = (g << p.gs) + (row & (p.G - 1));
+                    float m = kNegBig, s_max = kMasked, sum = 0.f;
+                    float4_t st[NW];
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) {
+                        st[w] = s_stat[w * kNarrow + row];
+                        if (st[w][1] != 0.f) m = fmaxf(m, st[w][0]);
+                        s_max = fmaxf(s_max, st[w][2]);
+                    }
+                    float4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int w = 0; w < NW; ++w) {
+                        const float f = st[w][1] != 0.f ? fast_exp2(st[w][0] - m) : 0.f;       // (a sum of NaN counts)
+                        if (f != 0.f) sum = fmaf(st[w][1], f, sum);
+                        const float4_t v = s_sum[(w * kNarrow + row) * 32 + ((c4 + row) & 31)];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], f, o[e]);
+                    }
+                    if (pieces == 1) {
+                        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                        *(half4_t*)(p.out + t * p.os_t + h * p.os_h + 4 * c4) = half4_t{(half_t)(o[0] * inv), (half_t)(o[1] * inv), (half_t)(o[2] * inv), (half_t)(o[3] * inv)};
+                        if (c4 == 0 && p.row_max) {
+                            p.row_max[h * p.st_h + t] = s_max * p.c1 * (1.f / kLog2e);
+                            p.row_sum[h * p.st_h + t] = sum == 0.f ? 0.f : sum * fast_exp2(fmaf(-s_max, p.c1, m));
+                        }
+                    } else {
+                        const int64_t at = slot * p.rows_cap + row;
+                        store_part(p.part_out + at * kD + 4 * c4, o[0], o[1]);
+                        store_part(p.part_out + at * kD + 4 * c4 + 2, o[2], o[3]);
+                        if (c4 == 0) {
+                            store_part(p.part_stat + 4 * at, m, sum);
+                            store_part(p.part_stat + 4 * at + 2, s_max, 0.f);
+                        }
+                    }
+                }
+                if (pieces > 1 && last_to_arrive(word, p.tag, pieces, &s_flag))
+                    for (int row = wave; row < rows; row += NW) merge_row(p, all, row, g, rq.t0 + (row >> p.gs), (g << p.gs) + (row & (p.G - 1)), lane);
+            } else {
+                wide_sums<NW, true>(sums, p, pc, span, s_all + At::tiles, &s_odd, s_place);
+                claim();
+                const int row = pc.row0 + 32 * wave + (lane & 31);
+                const bool active = pc.row0 + 32 * wave < rows;
+                bool mine = true;
+                if (pieces > 1) {
+                    if (active) store_wide(p, sums, slot, wave, lane);
+                    mine = last_to_arrive(word, p.tag, pieces, &s_flag);
+                    if (mine && active) merge_wide(p, sums, all, g, wave, lane);
+                }
+                if (mine && row < rows) write_row(p, sums, 0, rq.t0 + (row >> p.gs), (g << p.gs) + (row & (p.G - 1)), lane >> 5);
+            }
+            __syncthreads();                                        // LDS is free for the next piece
+        }
+        x = cur.unit ? x + n_shares : c0 + len;
+        if (x >= end) return;
+    }
+}
 
 }  // namespace
 
-// Key ranges, per KV head, that the plan aims at.
-static int64_t target_of(const Geom& g)
-{
-    const int64_t t = (512 + g.Hkv - 1) / g.Hkv;
-    return t < 1 ? 1 : t;
-}
+// Few long chunks: 8 waves read a key tile for 256 rows; many requests: 4 waves, two workgroups to a CU, one works while the other comes
+// or goes.  8 and 4 waves: a chunk of 2048 on 32768 keys 1.11 and 1.20 ms, 16 requests with 2048 tokens among them (500 for four of
+// them, one for the others) on up to 8192 keys 112 and 94 us, 64 requests of a token each on up to 32768 keys 178 and 180, one on 4096 16.8 and 15.7.
+static int waves_of(const Geom& g, int64_t T) { return T * g.G >= (int64_t)g.B * 1024 ? 8 : 4; }
+// Shares per KV head: the chip's workgroups, or one each.
+static int shares_of(const Geom& g, int nw) { return g.Hkv < kWaves / nw ? kWaves / nw / g.Hkv : 1; }
+// A batch has no block of more rows than it has itself.
+static int rows_cap_of(const Geom& g, int64_t T, int nw) { return T * g.G < 32 * nw ? ((int)(T * g.G) + 31) / 32 * 32 : 32 * nw; }
 
-// Rows of partial sums: a request with S > 1 ranges has S <= 2 tiles / each of them, and `each` is work / target or more, so that
-// all S x rows of one KV head come to twice target x the rows of a block at most, and a batch has no block of more rows than it has itself.
-static int64_t part_rows_of(const Geom& g, int64_t T)
-{
-    const int64_t wide = T * g.G < 256 ? T * g.G : 256;
-    return 2 * target_of(g) * wide * g.Hkv + 2 * g.Hkv * wide;
-}
-
+// What either would need: a workspace made for many tokens then does for fewer.
 size_t page_attn_workspace_bytes(const Geom& g, int64_t T)
 {
-    return align_up((size_t)T * sizeof(int4_t)) + (size_t)part_rows_of(g, T) * (sizeof(float4_t) + kD * sizeof(float));
+    size_t most = 0;
+    for (int nw = 4; nw <= 8; nw += 4) {
+        const size_t pairs = (size_t)shares_of(g, nw) * g.Hkv;
+        const size_t n = align_up(pairs * sizeof(unsigned long long)) + 2 * pairs * rows_cap_of(g, T, nw) * (kD + 4) * sizeof(float);
+        most = most < n ? n : most;
+    }
+    return most;
+}
+
+template <int NW>
+static hipError_t launch_t(const Geom& g, Params& p, int64_t T, void* ws, hipStream_t st)
+{
+    p.shares = shares_of(g, NW);
+    p.rows_cap = rows_cap_of(g, T, NW);
+    const int64_t pairs = (int64_t)p.shares * g.Hkv;
+    p.tag = next_launch_tag();
+    p.done = (unsigned long long*)ws;
+    p.part_out = (float*)((char*)ws + align_up((size_t)pairs * sizeof(unsigned long long)));
+    p.part_stat = p.part_out + 2 * pairs * p.rows_cap * kD;
+    // a workgroup per share, or, if there can be so many, per block
+    const int64_t most = T * g.G / (32 * NW) + (g.B < T ? g.B : T);
+    const int64_t grid = most * g.Hkv >= kBlocksEach * (kWaves / NW) && most > p.shares ? most : p.shares;
+    hipLaunchKernelGGL(page_attn_kernel<NW>, dim3((unsigned)(grid * g.Hkv)), dim3(NW * 64), 0, st, p);
+    return hipGetLastError();
 }
 
 hipError_t launch_page_attn(const Geom& g, const Pages& pg, const PageAttnArgs& a, void* ws, hipStream_t st)
@@ -672,34 +653,8 @@ hipError_t launch_page_attn(const Geom& g, const Pages& pg, const PageAttnArgs& 
     p.qs_t = a.qs_t; p.qs_h = a.qs_h; p.os_t = (int64_t)g.Hq * kD; p.os_h = kD; p.st_h = a.T;
     p.c1 = a.scale * kLog2e; p.Hkv = g.Hkv; p.G = g.G; p.gs = log2_of(g.G); p.window = a.window; p.n_sink = a.n_sink;
     p.q_start = a.q_start; p.ctx_len = a.ctx_len; p.table = a.table; p.table_cap = a.table_cap; p.n_pages = pg.n;
-    p.T = (int)a.T; p.R = g.B; p.shift = pg.shift; p.target = (int)target_of(g);
-    p.part_rows = part_rows_of(g, a.T);
-    p.plan = (int4_t*)ws;
-    p.part_stat = (float4_t*)((char*)ws + align_up((size_t)a.T * sizeof(int4_t)));
-    p.part_out = (float*)(p.part_stat + p.part_rows);
-    const int64_t rows = a.T * g.G, some = g.B < a.T ? g.B : a.T;
-    auto grid = [&](int nw) { return (p.target + rows / (32 * nw) + some + 1) * g.Hkv; };
-    const bool wide = rows * g.Hkv >= 256 * 64;
-    const hipError_t e = wide ? launch_t<8, true>(p, grid(8), st) : launch_t<4, true>(p, grid(4), st);
-    if (e != hipSuccess) return e;
-    const int64_t n = a.T * g.Hq;
-    hipLaunchKernelGGL(merge_kernel, dim3((unsigned)((n + kMergeThreads / 64 - 1) / (kMergeThreads / 64))), dim3(kMergeThreads), 0, st, p, (int)n);
-    return hipGetLastError();
-}
-
-hipError_t launch_prefill_attn_window(const Geom& g, const half_t* q, const half_t* k, const half_t* v, int64_t N, int64_t Nq, float scale,
-                                      int window, int n_sink, half_t* out, float* row_max, float* row_sum, hipStream_t st)
-{
-    Params p = {};
-    p.q = q; p.k = k; p.v = v; p.out = out; p.row_max = row_max; p.row_sum = row_sum;
-    p.qs_t = p.os_t = kD; p.qs_h = p.os_h = Nq * kD; p.qs_b = p.os_b = g.Hq * Nq * kD; p.st_h = Nq; p.st_b = g.Hq * Nq;
-    p.c1 = scale * kLog2e; p.Hkv = g.Hkv; p.G = g.G; p.gs = log2_of(g.G); p.window = window; p.n_sink = n_sink;
-    p.N = (int)N; p.Nq = (int)Nq;
-    const int64_t pairs = (int64_t)g.B * g.Hkv, rows = Nq * g.G;
-    const bool wide = (rows + 255) / 256 * pairs >= 384;
-    const int span = wide ? 256 : 128;
-    p.q_blocks = (int)((rows + span - 1) / span);
-    return wide ? launch_t<8, false>(p, p.q_blocks * pairs, st) : launch_t<4, false>(p, p.q_blocks * pairs, st);
+    p.T = (int)a.T; p.R = g.B; p.shift = pg.shift;
+    return waves_of(g, a.T) == 8 ? launch_t<8>(g, p, a.T, ws, st) : launch_t<4>(g, p, a.T, ws, st);
 }
 
 }  // namespace antkv

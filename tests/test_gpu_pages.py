@@ -242,7 +242,7 @@ class Cache:
             self.v_pages[ids, :, j % self.page] = self.v[r].transpose(0, 1)
 
 
-def check_attn(c, new, Hq, window=0, n_sink=0, q=None, pad=0, seed=1, scale=SCALE, hidden=None, workspace=None, ctx=None):
+def check_attn(c, new, Hq, window=0, n_sink=0, q=None, pad=0, seed=1, scale=SCALE, hidden=None, workspace=None, ctx=None, each=1):
     """Every row of the batch against 64 bits; rows behind the last request stay as they are."""
     Hkv, R, T = c.k_pages.shape[1], len(new), sum(new) + pad
     G = Hq // Hkv
@@ -259,7 +259,7 @@ def check_attn(c, new, Hq, window=0, n_sink=0, q=None, pad=0, seed=1, scale=SCAL
     for r, n in enumerate(new):
         a, b = int(starts[r]), int(starts[r + 1])
         pos = torch.arange((ctx or c.ctx)[r] - n, (ctx or c.ctx)[r], device="cuda")
-        for h in range(Hq if n else 0):
+        for h in range(0, Hq if n else 0, each):
             want = exact(q[a:b, h], c.k[r][h // G], c.v[r][h // G], pos, window, n_sink, scale, None if hidden is None else hidden[r])
             compare((out[a:b, h], top[h, a:b], total[h, a:b]), want, f"request {r}, head {h}")
     return out
@@ -300,6 +300,15 @@ def test_page_attn_wide_batch():
     """Enough rows for workgroups of eight waves; requests of one token among long chunks."""
     check_attn(Cache(9, [1500, 900, 2000, 1, 400], 8, 32), [1500, 1, 300, 1, 0], 32, pad=5)
     check_attn(Cache(9, [1500, 900, 2000, 1, 400], 8, 32), [1500, 1, 300, 1, 0], 32, window=200, n_sink=5)
+
+
+def test_page_attn_a_workgroup_per_block():
+    """So many blocks that none of them is cut: many requests of few tokens, and a long prompt."""
+    rng = np.random.default_rng(4)
+    ctx = rng.integers(1, 300, 300).tolist()
+    check_attn(Cache(6, ctx, 8, 16), [1 + (r % 7 == 0) * min(c - 1, 40) for r, c in enumerate(ctx)], 16, each=3)
+    check_attn(Cache(7, [8300, 40], 8, 64), [8250, 1], 32, each=7)
+    check_attn(Cache(7, [8300, 40], 8, 64), [8250, 1], 32, window=700, n_sink=40, each=7)
 
 
 def test_page_attn_scores_far_apart():

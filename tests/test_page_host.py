@@ -72,7 +72,7 @@ def _attn(lib, g=None, q=FAKE, qt=1024, qh=128, T=4, qs=FAKE, ctx=FAKE, table=FA
 
 
 @pytest.mark.parametrize("bad,code", [
-    (dict(g=_g(Hq=16)), EUNSUPPORTED), (dict(g=_g(Hq=7)), EINVAL), (dict(page=17), EUNSUPPORTED), (dict(n_pages=-1), EINVAL), (dict(T=-1), EINVAL),
+    (dict(g=_g(Hq=16)), EUNSUPPORTED), (dict(g=_g(Hq=7)), EINVAL), (dict(g=_g(B=8193)), EUNSUPPORTED), (dict(page=17), EUNSUPPORTED), (dict(n_pages=-1), EINVAL), (dict(T=-1), EINVAL),
     (dict(T=1 << 28), EINVAL), (dict(cap=0), EINVAL), (dict(cap=1 << 27), EINVAL), (dict(window=-1), EINVAL), (dict(window=(1 << 30) + 1), EINVAL), (dict(sink=-1), EINVAL),
     (dict(scale=0.0), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(rm=FAKE), EINVAL), (dict(rs=FAKE), EINVAL), (dict(q=None), EINVAL),
     (dict(q=ODD), EINVAL), (dict(out=ODD), EINVAL), (dict(kp=ODD), EINVAL), (dict(qs=None), EINVAL), (dict(ctx=None), EINVAL), (dict(table=None), EINVAL),
@@ -85,8 +85,10 @@ def test_page_attn_refusals(lib, bad, code):
 def test_page_attn_workspace(lib):
     need = lambda g, T: lib.antkv_page_attn_workspace(ctypes.byref(g), T)
     assert need(_g(D=64), 4) == 0 and need(_g(), 0) == 0 and need(_g(B=0), 4) == 0 and need(_g(), 1 << 30) == 0
-    sizes = [need(_g(), T) for T in (1, 2, 63, 64, 65, 1000, 100000)]
-    assert sizes == sorted(sizes) and sizes[0] > 0                  # more tokens never need less
+    for hkv in (1, 2, 7, 8, 100, 300, 600):
+        sizes = [need(_g(B=3, Hq=4 * hkv, Hkv=hkv), T) for T in (1, 2, 31, 63, 64, 65, 255, 700, 768, 1000, 100000)]
+        assert sizes == sorted(sizes) and sizes[0] > 0              # more tokens never need less
+    sizes = [need(_g(), T) for T in (1, 100000)]
     assert sizes[-1] < 300 << 20                                    # partial sums of the cut requests, not of every row
     assert _attn(lib, T=4, wsb=need(_g(), 4) - 1) == EWORKSPACE
 
