@@ -404,22 +404,26 @@ def decode_attn_static(geom: Geometry, q: torch.Tensor, scale: float, codes_k: t
 
 
 # ---- the FP16 cache in pages, and windowed prompts ----------------------------------------------------------------------
+# Host cost of a call: checks by keyword arguments and generators took 4 of the 9.8 us of a page_store call and, with four outputs
+# allocated one by one, 9 of the 15 us of page_map.  Each check now asks first whether all is well.
 
-def _same_device(first: torch.Tensor, **others):
-    """Every tensor on the first one's device, which is made current for the launch if it is not: the returned number, or None."""
-    at = first.get_device()
-    for name, t in others.items():
-        if t is not None and t.get_device() != at:
-            raise ValueError(f"{name} must be on the device of the other tensors")
-    return None if torch.cuda.current_device() == at else at
-
-
-def _launch(call, what: str, device, *args):
-    if device is None:
-        _check(call(*args), what)
+def _run(call, what: str, device: int, *args):
+    """The call on `device`, which is made current for it if it is not."""
+    if torch._C._cuda_getDevice() == device:
+        rc = call(*args)
     else:
         with torch.cuda.device(device):
-            _check(call(*args), what)
+            rc = call(*args)
+    if rc != 0:
+        raise AntkvError(rc, what)
+
+
+def _one_device(*tensors) -> int:
+    at = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError("all tensors must be on the same device")
+    return at
 
 
 def _rows(t: torch.Tensor, name: str, heads: int):
@@ -428,22 +432,30 @@ def _rows(t: torch.Tensor, name: str, heads: int):
         raise ValueError(f"{name} must be a device tensor")
     if t.dtype is not torch.float16:
         raise TypeError(f"{name} must be torch.float16")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128 or t.stride(2) != 1:
+    if t.dim() != 3 or t.shape[1:] != (heads, 128) or t.stride(2) != 1:
         raise ValueError(f"{name} must be [T, {heads}, 128] with contiguous channels")
 
 
 def _pools(k_pages: torch.Tensor, v_pages: torch.Tensor, heads: int):
     _need(k_pages, torch.float16, "k_pages")
     _need(v_pages, torch.float16, "v_pages")
-    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.shape[1] != heads or k_pages.shape[3] != 128:
+    shape = k_pages.shape
+    if len(shape) != 4 or shape[1] != heads or shape[3] != 128 or v_pages.shape != shape:
         raise ValueError(f"k_pages and v_pages must be [n_pages, {heads}, page_size, 128]")
-    return k_pages.shape[0], k_pages.shape[2]
+    return shape[0], shape[2]
 
 
-def _ints(t: torch.Tensor, name: str, *shape):
+def _ints(t: torch.Tensor, name: str, shape: tuple):
     _need(t, torch.int32, name)
-    if t.dim() != len(shape) or any(n is not None and t.shape[i] != n for i, n in enumerate(shape)):
-        raise ValueError(f"{name} must be int32 {list('*' if n is None else n for n in shape)}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {list(shape)}")
+
+
+def _table(t: torch.Tensor, requests: int) -> int:
+    _need(t, torch.int32, "table")
+    if t.dim() != 2 or t.shape[0] != requests:
+        raise ValueError(f"table must be [{requests}, entries]")
+    return t.shape[1]
 
 
 def prefill_attn_window(geom: Geometry, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, window: int, n_sink: int = 0,
@@ -453,16 +465,19 @@ def prefill_attn_window(geom: Geometry, q: torch.Tensor, k: torch.Tensor, v: tor
     _need(q, torch.float16, "q")
     _need(k, torch.float16, "k")
     _need(v, torch.float16, "v")
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q, k and v must have four dimensions")
     B, Hq, Nq, D = q.shape
     N = k.shape[2]
     if (B, Hq, D) != (geom.B, geom.Hq, geom.D) or k.shape != (B, geom.Hkv, N, D) or v.shape != k.shape:
         raise ValueError("q, k and v do not fit the geometry")
-    device = _same_device(q, k=k, v=v)
-    out = torch.empty((B, Hq, Nq, D), dtype=torch.float16, device=q.device)
-    row_max = torch.empty((B, Hq, Nq), dtype=torch.float32, device=q.device) if want_stats else None
-    row_sum = torch.empty((B, Hq, Nq), dtype=torch.float32, device=q.device) if want_stats else None
-    _launch(load_library().antkv_prefill_attn_window, "antkv_prefill_attn_window", device, geom._c, _p(q), _p(k), _p(v), N, Nq, float(scale),
-            int(window), int(n_sink), _p(out), _p(row_max), _p(row_sum), _stream(q))
+    device = _one_device(q, k, v)
+    out = torch.empty_like(q)
+    row_max = row_sum = None
+    if want_stats:
+        row_max, row_sum = torch.empty((2, B, Hq, Nq), dtype=torch.float32, device=q.device).unbind(0)
+    _run(load_library().antkv_prefill_attn_window, "antkv_prefill_attn_window", device, geom._c, q.data_ptr(), k.data_ptr(), v.data_ptr(), N, Nq,
+         float(scale), int(window), int(n_sink), out.data_ptr(), _p(row_max), _p(row_sum), _stream(q))
     return out, row_max, row_sum
 
 
@@ -471,41 +486,46 @@ def page_map(held_len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor,
     """antkv_page_map: held_len, new_len int32 [R], table int32 [R,cap] (new entries are written), free_pages int32 [n] ->
     (ctx_len int32 [R], q_start int32 [R+1], slot int32 [T], status int32 [2]).  `out`: such a tuple, to be written again."""
     R = held_len.shape[0]
-    _ints(held_len, "held_len", R)
-    _ints(new_len, "new_len", R)
-    _ints(table, "table", R, None)
-    _ints(free_pages, "free_pages", None)
+    _ints(held_len, "held_len", (R,))
+    _ints(new_len, "new_len", (R,))
+    cap = _table(table, R)
+    _need(free_pages, torch.int32, "free_pages")
     if free_at is not None:
         _need(free_at, torch.int32, "free_at")
         if free_at.numel() < 1:
             raise ValueError("free_at must hold a number")
-    dev = table.device
     if out is None:
-        out = tuple(torch.empty(n, dtype=torch.int32, device=dev) for n in (R, R + 1, T, 2))
+        slot, ctx_len, q_start, status = table.new_empty(T + 2 * R + 3).split_with_sizes((T, R, R + 1, 2))
+        out = ctx_len, q_start, slot, status
+        device = _one_device(table, held_len, new_len, free_pages, free_at)
     else:
-        for t, name, n in zip(out, ("ctx_len", "q_start", "slot", "status"), (R, R + 1, T, 2)):
-            _ints(t, name, n)
-    ctx_len, q_start, slot, status = out
-    device = _same_device(table, held_len=held_len, new_len=new_len, free_pages=free_pages, free_at=free_at, ctx_len=ctx_len, q_start=q_start,
-                          slot=slot, status=status)
-    _launch(load_library().antkv_page_map, "antkv_page_map", device, R, _p(held_len), _p(new_len), _p(table), table.shape[1], n_pages, page_size,
-            _p(free_pages), free_pages.shape[0], _p(free_at), T, _p(ctx_len), _p(q_start), _p(slot), _p(status), _stream(table))
+        ctx_len, q_start, slot, status = out
+        _ints(ctx_len, "ctx_len", (R,))
+        _ints(q_start, "q_start", (R + 1,))
+        _ints(slot, "slot", (T,))
+        _ints(status, "status", (2,))
+        device = _one_device(table, held_len, new_len, free_pages, free_at, *out)
+    _run(load_library().antkv_page_map, "antkv_page_map", device, R, held_len.data_ptr(), new_len.data_ptr(), table.data_ptr(), cap, n_pages, page_size,
+         free_pages.data_ptr(), free_pages.numel(), _p(free_at), T, ctx_len.data_ptr(), q_start.data_ptr(), slot.data_ptr(), status.data_ptr(),
+         _stream(table))
     return out
 
 
 def page_store(geom: Geometry, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor) -> None:
     """antkv_page_store: rows of k, v fp16 [T,Hkv,D] (equal strides, channels contiguous) to slot int32 [T] of the pools
     fp16 [n_pages,Hkv,page_size,D]."""
-    _rows(k, "k", geom.Hkv)
-    _rows(v, "v", geom.Hkv)
-    n_pages, page_size = _pools(k_pages, v_pages, geom.Hkv)
+    heads = geom.Hkv
+    _rows(k, "k", heads)
+    n_pages, page_size = _pools(k_pages, v_pages, heads)
     T = k.shape[0]
-    if v.shape[0] != T or (T > 1 and v.stride(0) != k.stride(0)) or (geom.Hkv > 1 and v.stride(1) != k.stride(1)):
-        raise ValueError("k and v must have the same shape and strides")
-    _ints(slot, "slot", T)
-    device = _same_device(k_pages, v_pages=v_pages, k=k, v=v, slot=slot)
-    _launch(load_library().antkv_page_store, "antkv_page_store", device, geom._c, _p(k), _p(v), k.stride(0) if T > 1 else 0,
-            k.stride(1) if geom.Hkv > 1 else 0, T, _p(slot), _p(k_pages), _p(v_pages), n_pages, page_size, _stream(k_pages))
+    if v.shape != k.shape or v.stride() != k.stride() or v.dtype is not torch.float16:
+        _rows(v, "v", heads)
+        if v.shape[0] != T or (T > 1 and v.stride(0) != k.stride(0)) or (heads > 1 and v.stride(1) != k.stride(1)):
+            raise ValueError("k and v must have the same shape and strides")
+    _ints(slot, "slot", (T,))
+    _run(load_library().antkv_page_store, "antkv_page_store", _one_device(k_pages, v_pages, k, v, slot), geom._c, k.data_ptr(), v.data_ptr(),
+         k.stride(0) if T > 1 else 0, k.stride(1) if heads > 1 else 0, T, slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_size,
+         _stream(k_pages))
 
 
 def page_load(geom: Geometry, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, N: int, first: int = 0,
@@ -513,26 +533,28 @@ def page_load(geom: Geometry, k_pages: torch.Tensor, v_pages: torch.Tensor, tabl
     """antkv_page_load: positions first .. first + N - 1 of the table's requests -> (k, v) fp16 [B,Hkv,N,D].  Rows at or behind
     ctx_len (int32 [B]) are left as they are: zeros where k and v are made here."""
     n_pages, page_size = _pools(k_pages, v_pages, geom.Hkv)
-    _ints(table, "table", geom.B, None)
+    cap = _table(table, geom.B)
     if ctx_len is not None:
-        _ints(ctx_len, "ctx_len", geom.B)
+        _ints(ctx_len, "ctx_len", (geom.B,))
     shape = (geom.B, geom.Hkv, N, geom.D)
     if k is None:
         k = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
     if v is None:
         v = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
-    for t, name in ((k, "k"), (v, "v")):
-        _need(t, torch.float16, name)
-        if t.shape != shape:
-            raise ValueError(f"{name} must be {list(shape)}")
-    device = _same_device(k_pages, v_pages=v_pages, table=table, ctx_len=ctx_len, k=k, v=v)
-    _launch(load_library().antkv_page_load, "antkv_page_load", device, geom._c, _p(k_pages), _p(v_pages), n_pages, page_size, _p(table),
-            table.shape[1], _p(ctx_len), first, N, _p(k), _p(v), geom.Hkv * N * geom.D, N * geom.D, geom.D, _stream(k_pages))
+    _need(k, torch.float16, "k")
+    _need(v, torch.float16, "v")
+    if k.shape != shape or v.shape != shape:
+        raise ValueError(f"k and v must be {list(shape)}")
+    rows = N * geom.D
+    _run(load_library().antkv_page_load, "antkv_page_load", _one_device(k_pages, v_pages, table, ctx_len, k, v), geom._c, k_pages.data_ptr(),
+         v_pages.data_ptr(), n_pages, page_size, table.data_ptr(), cap, _p(ctx_len), first, N, k.data_ptr(), v.data_ptr(), geom.Hkv * rows, rows,
+         geom.D, _stream(k_pages))
     return k, v
 
 
 def page_attn_workspace(geom: Geometry, T: int, device) -> torch.Tensor:
-    """A workspace of antkv_page_attn_workspace(geom, T) bytes for page_attn, for calls that follow each other on one stream."""
+    """A workspace of antkv_page_attn_workspace(geom, T) bytes for page_attn, for calls that follow each other on one stream with up to
+    T rows."""
     return _workspace(load_library().antkv_page_attn_workspace(geom._c, T), device)
 
 
@@ -542,25 +564,28 @@ def page_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Tens
     """antkv_page_attn: q fp16 [T,Hq,D] (channels contiguous), q_start int32 [R+1], ctx_len int32 [R], table int32 [R,cap], pools
     fp16 [n_pages,Hkv,page_size,D], geom.B = R -> (out fp16 [T,Hq,D], row_max, row_sum fp32 [Hq,T] or None).
     Rows of out behind q_start[R] are left as they are (undefined where out is made here)."""
-    _rows(q, "q", geom.Hq)
+    Hq, R = geom.Hq, geom.B
+    _rows(q, "q", Hq)
     n_pages, page_size = _pools(k_pages, v_pages, geom.Hkv)
-    T, R = q.shape[0], geom.B
-    _ints(q_start, "q_start", R + 1)
-    _ints(ctx_len, "ctx_len", R)
-    _ints(table, "table", R, None)
-    dev = q.device
+    T = q.shape[0]
+    _ints(q_start, "q_start", (R + 1,))
+    _ints(ctx_len, "ctx_len", (R,))
+    cap = _table(table, R)
     if out is None:
-        out = torch.empty((T, geom.Hq, 128), dtype=torch.float16, device=dev)
+        out = k_pages.new_empty((T, Hq, 128))
     else:
         _need(out, torch.float16, "out")
         if out.shape != q.shape:
             raise ValueError("out must have the shape of q")
-    row_max = torch.empty((geom.Hq, T), dtype=torch.float32, device=dev) if want_stats else None
-    row_sum = torch.empty((geom.Hq, T), dtype=torch.float32, device=dev) if want_stats else None
+    row_max = row_sum = None
+    if want_stats:
+        row_max, row_sum = torch.empty((2, Hq, T), dtype=torch.float32, device=q.device).unbind(0)
     if workspace is None:
-        workspace = page_attn_workspace(geom, T, dev)
-    device = _same_device(q, k_pages=k_pages, v_pages=v_pages, q_start=q_start, ctx_len=ctx_len, table=table, out=out, workspace=workspace)
-    _launch(load_library().antkv_page_attn, "antkv_page_attn", device, geom._c, _p(q), q.stride(0) if T > 1 else 0,
-            q.stride(1) if geom.Hq > 1 else 0, T, _p(q_start), _p(ctx_len), _p(table), table.shape[1], _p(k_pages), _p(v_pages), n_pages,
-            page_size, float(scale), int(window), int(n_sink), _p(out), _p(row_max), _p(row_sum), _p(workspace), workspace.numel(), _stream(q))
+        workspace = page_attn_workspace(geom, T, q.device)
+    else:
+        _need(workspace, torch.uint8, "workspace")
+    _run(load_library().antkv_page_attn, "antkv_page_attn", _one_device(q, k_pages, v_pages, q_start, ctx_len, table, out, workspace), geom._c,
+         q.data_ptr(), q.stride(0) if T > 1 else 0, q.stride(1) if Hq > 1 else 0, T, q_start.data_ptr(), ctx_len.data_ptr(), table.data_ptr(), cap,
+         k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_size, float(scale), int(window), int(n_sink), out.data_ptr(), _p(row_max), _p(row_sum),
+         workspace.data_ptr(), workspace.numel(), _stream(q))
     return out, row_max, row_sum

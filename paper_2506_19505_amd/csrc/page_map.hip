@@ -2,10 +2,10 @@
 //
 // Two prefix sums over the requests say everything: of the new tokens (where a request's rows start in the packed batch) and of
 // the pages it takes (where its pages start in the list of free ones).  Every workgroup makes both for itself (8 bytes a request,
-// out of the L2) and keeps them in LDS; it then writes its share of the slots, four to a thread, and of the new table entries.  A
+// out of the L2) and keeps them in LDS, with the lengths; it then writes its share of the slots, and of the new table entries.  A
 // slot in a new page comes from the free list, one in a page held before from an entry that no thread writes: one launch, nothing
 // to wait for between workgroups.
-// Bound: latency, a launch and three dependent loads.
+// Bound: latency, a launch and two dependent loads (256 requests of a token each 4.3 us, 48 prompts of 65536 tokens 5.0).
 #include "common.h"
 
 namespace antkv {
@@ -13,7 +13,6 @@ namespace antkv {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kPer = 4;                                             // slots of a thread
 constexpr int64_t kMost = 0x7fffffffLL;
 
 struct MapParams {
@@ -35,35 +34,47 @@ __device__ __forceinline__ int last_at_most(const int* s, int n, int x)
     return lo;
 }
 
+// inclusive sum over the wave (register moves between lanes: within rows of 16, then across them)
+template <int kCtrl, int kMask>
+__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, kCtrl, kMask, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += from_lane<0x111, 0xf>(x);
+    x += from_lane<0x112, 0xf>(x);
+    x += from_lane<0x114, 0xf>(x);
+    x += from_lane<0x118, 0xf>(x);
+    x += from_lane<0x142, 0xa>(x);
+    return x + from_lane<0x143, 0xc>(x);
+}
+// of 31-bit numbers, in halves that cannot overflow
+__device__ __forceinline__ int64_t wave_scan31(int x) { return ((int64_t)wave_scan(x >> 16) << 16) + wave_scan(x & 0xffff); }
+
+template <int kPer>                                     // slots of a thread: 4 where a request has many, which then are of one or two pages
 __global__ __launch_bounds__(kThreads) void page_map_kernel(const MapParams p)
 {
-    extern __shared__ int s_pre[];                                  // [R + 1] first tokens, [R + 1] first pages of the free list
+    extern __shared__ int s_pre[];                                  // [R + 1] first tokens, [R + 1] first pages of the free list, [R] lengths
     __shared__ int64_t s_wave[2][kWaves];
     __shared__ int s_short;
     int* s_tok = s_pre;
     int* s_page = s_pre + p.R + 1;
+    int* s_held = s_page + p.R + 1;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t size = 1ll << p.shift;
     const int64_t at0 = p.free_at ? (*p.free_at > 0 ? *p.free_at : 0) : 0;
     if (tid == 0) s_short = 0;
 
-    auto held_of = [&](int r) { const int64_t h = p.held[r]; return h > 0 ? h : 0; };
     auto has = [&](int64_t h) { const int64_t n = (h + size - 1) >> p.shift; return n < p.table_cap ? n : p.table_cap; };
     int64_t run_tok = 0, run_page = 0;
     for (int base = 0; base < p.R; base += kThreads) {
         const int r = base + tid;
         int64_t n = 0, take = 0;
         if (r < p.R) {
-            const int64_t h = held_of(r);
-            n = p.fresh[r] > 0 ? p.fresh[r] : 0;
+            const int u = p.held[r], v = p.fresh[r], h = u > 0 ? u : 0;
+            s_held[r] = h;
+            n = v > 0 ? v : 0;
             take = has(h + n) - has(h);
         }
-        int64_t a = n, b = take;                                    // inclusive sums over the wave
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int64_t u = __shfl_up(a, off, 64), v = __shfl_up(b, off, 64);
-            if (lane >= off) { a += u; b += v; }
-        }
+        int64_t a = wave_scan31((int)n), b = wave_scan31((int)take);
         if (lane == 63) { s_wave[0][wave] = a; s_wave[1][wave] = b; }
         __syncthreads();
         int64_t all_tok = 0, all_page = 0;
@@ -117,7 +128,7 @@ __global__ __launch_bounds__(kThreads) void page_map_kernel(const MapParams p)
             if (i == 0 || t + i >= next) {
                 r = last_at_most(s_tok, p.R, (int)(t + i));
                 next = s_tok[r + 1];
-                h = held_of(r);
+                h = s_held[r];
                 pi = -1;
             }
             const int64_t pos = h + (t + i - s_tok[r]);
@@ -127,7 +138,8 @@ __global__ __launch_bounds__(kThreads) void page_map_kernel(const MapParams p)
             }
             if (page >= 0) out[i] = (int)((page << p.shift) + (pos & (size - 1)));
         }
-        if (t + kPer <= p.T_cap && ((uintptr_t)p.slot & 15) == 0) *(int4_t*)(p.slot + t) = int4_t{out[0], out[1], out[2], out[3]};
+        if (kPer == 4 && t + kPer <= p.T_cap && ((uintptr_t)p.slot & 15) == 0)
+            *(int4_t*)(p.slot + t) = int4_t{out[0], out[1 % kPer], out[2 % kPer], out[3 % kPer]};
         else
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
@@ -137,13 +149,13 @@ __global__ __launch_bounds__(kThreads) void page_map_kernel(const MapParams p)
     const int pages = s_page[p.R];
     for (int64_t i = (int64_t)blockIdx.x * kThreads + tid; i < pages; i += (int64_t)gridDim.x * kThreads) {
         const int r = last_at_most(s_page, p.R, (int)i);
-        p.table[(int64_t)r * p.table_cap + has(held_of(r)) + (i - s_page[r])] = (int)from_list(i);
+        p.table[(int64_t)r * p.table_cap + has(s_held[r]) + (i - s_page[r])] = (int)from_list(i);
     }
     // lengths, starts, what is left
     if (blockIdx.x != 0) return;
     int missing = 0;
     for (int r = tid; r < p.R; r += kThreads) {
-        const int64_t h = held_of(r), n = p.fresh[r] > 0 ? p.fresh[r] : 0, ctx = h + n;
+        const int64_t h = s_held[r], n = p.fresh[r] > 0 ? p.fresh[r] : 0, ctx = h + n;
         p.ctx_len[r] = (int)(ctx < kMost ? ctx : kMost);
         p.q_start[r] = s_tok[r];
         if (n > 0) {
@@ -173,17 +185,21 @@ hipError_t launch_page_map(const Pages& pg, int R, const int32_t* held, const in
     p.held = held; p.fresh = fresh; p.free_pages = free_pages; p.free_at = free_at;
     p.table = table; p.ctx_len = ctx_len; p.q_start = q_start; p.slot = slot; p.status = status;
     p.table_cap = table_cap; p.n_pages = pg.n; p.n_free = n_free; p.T_cap = T_cap; p.R = R; p.shift = pg.shift;
-    int64_t blocks = (T_cap + kThreads * kPer - 1) / (kThreads * kPer);
-    if (blocks < 1) blocks = 1;
-    if (blocks > 1024) blocks = 1024;
-    const size_t lds = 2 * (size_t)(R + 1) * sizeof(int);
-    if (lds > 60 * 1024) {
-        static OncePerDevice once;
-        const hipError_t e = allow_lds(once, (const void*)page_map_kernel, 2 * (kMapRequests + 1) * sizeof(int));
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL(page_map_kernel, dim3((unsigned)blocks), dim3(kThreads), lds, st, p);
-    return hipGetLastError();
+    auto launch = [&](const void* at, auto kernel, int per, OncePerDevice& once) {
+        int64_t blocks = (T_cap + kThreads * per - 1) / (kThreads * per);
+        if (blocks < 1) blocks = 1;
+        if (blocks > 1024) blocks = 1024;
+        const size_t lds = (3 * (size_t)R + 2) * sizeof(int);
+        if (lds > 60 * 1024) {
+            const hipError_t e = allow_lds(once, at, (3 * (size_t)kMapRequests + 2) * sizeof(int));
+            if (e != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), lds, st, p);
+        return hipGetLastError();
+    };
+    static OncePerDevice once1, once4;
+    return T_cap >= 8 * (int64_t)R ? launch((const void*)page_map_kernel<4>, page_map_kernel<4>, 4, once4)
+                                   : launch((const void*)page_map_kernel<1>, page_map_kernel<1>, 1, once1);
 }
 
 }  // namespace antkv
