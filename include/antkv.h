@@ -351,8 +351,8 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
  * Rows of T behind q_start[R] are left as they are.  Keys on pages that are none, and positions behind the table's end, are not
  * seen; a row that sees nothing is zero, with row_max -inf and row_sum 0.  What a row does not see has no influence on it, whatever it
  * holds (pages need not be cleared).  Sums have a fixed order: equal inputs give equal bits.
- * The workspace size is a function of Hq, Hkv, R and T; calls that share a workspace must not overlap.
- * Errors: EINVAL, EUNSUPPORTED, EWORKSPACE, ELAUNCH.
+ * n_pages * Hkv * page_size below 2^32.  The workspace size is a function of Hq, Hkv, R and T; calls that share a workspace must not
+ * overlap.  Errors: EINVAL, EUNSUPPORTED, EWORKSPACE, ELAUNCH.
  */
 size_t antkv_page_attn_workspace(const antkv_geom* geom, int64_t T);
 int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t qs_h, int64_t T, const int32_t* q_start,

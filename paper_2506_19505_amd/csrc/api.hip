@@ -383,7 +383,7 @@ int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t
     if (rc) return rc;
     if (g.B > kMapRequests) return ANTKV_EUNSUPPORTED;
     if (T < 0 || T > 0x7fffffffLL / g.Hq || bad_table(table_cap, pg) || window < 0 || window > 1LL << 30 || n_sink < 0) return ANTKV_EINVAL;
-    if (n_pages * g.Hkv > 0x7fffffffLL / (page_size / 16)) return ANTKV_EINVAL;
+    if (n_pages * g.Hkv > 0x0fffffffLL / (page_size / 16)) return ANTKV_EINVAL;      // places of 16 rows: below 2^28, 1 TB
     if ((row_max == nullptr) != (row_sum == nullptr) || !(scale > 0.f)) return ANTKV_EINVAL;
     if (T == 0 || g.B == 0) return ANTKV_OK;
     if (!q || !q_start || !ctx_len || !table || !k_pages || !v_pages || !out) return ANTKV_EINVAL;

@@ -22,6 +22,7 @@ namespace {
 using namespace span;
 
 constexpr int kNarrow = 32;
+constexpr int kTurnNarrow = 1024;                                   // key tiles of a narrow block whose pages are looked up at a time
 constexpr int kWindow = 64;                                         // requests that a wave looks at at a time
 constexpr int kWindows = kMapRequests / kWindow;
 constexpr int kBlocksEach = 4;
@@ -30,10 +31,10 @@ constexpr int kWaves = 2048;                                        // that the 
 template <int NW>                                       // waves of a workgroup: 8 or 4
 struct Lds {
     static constexpr int tiles = 0;                                 // narrow: a K and a V tile per wave; wide: the rings
-    static constexpr int place = NW * 2 * kTileBytes;               // [kTurn][2]: places of the turn's key tiles
-    static constexpr int stat = place + kTurn * 8;                  // [NW][kNarrow][4]: reference, sum, largest score
+    static constexpr int notes = NW * 2 * kTileBytes;               // what is known of the turn's key tiles; narrow: [kTurnNarrow][2] places
+    static constexpr int stat = notes + kNotes * (int)sizeof(Note); // [NW][kNarrow][4]: reference, sum, largest score
     static constexpr int total = stat + NW * kNarrow * 16;
-    static_assert(kRingBytes <= place && (total + kWindows * 8 + 1024) * (8 / NW) <= 163840, "LDS of a CU");
+    static_assert(kRingBytes <= notes && kTurnNarrow * 8 <= stat - notes && (total + kWindows * 8 + 1024) * (8 / NW) <= 163840, "LDS of a CU");
 };
 
 __device__ __forceinline__ Request request_of(const Params& p, int r)
@@ -155,8 +156,8 @@ __device__ __forceinline__ void narrow_sums(Sums& sums, const Params& p, const P
     const Operands at(k_at, v_at, lane);
     half8_t tq[8];
     load_query(tq, p, x, row, lane);
-    for (int ua = x.from; ua < x.to; ua += kTurn) {
-        const int m = x.to - ua < kTurn ? x.to - ua : kTurn;
+    for (int ua = x.from; ua < x.to; ua += kTurnNarrow) {
+        const int m = x.to - ua < kTurnNarrow ? x.to - ua : kTurnNarrow;
         const int32_t* row_of = p.table + (int64_t)x.r * p.table_cap;
         if (ua > x.from) __syncthreads();                           // the turn before has been read
         for (int k = tid; k < 2 * m; k += NW * 64) {
@@ -397,7 +398,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
     using At = Lds<NW>;
     __shared__ __attribute__((aligned(1024))) unsigned char s_all[At::total];
     __shared__ int s_cost[kWindows], s_blocks[kWindows], s_odd, s_flag;
-    int* s_place = (int*)(s_all + At::place);
+    Note* s_notes = (Note*)(s_all + At::notes);
     float4_t* s_stat = (float4_t*)(s_all + At::stat);
     const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6);
     const int share = blockIdx.x / p.Hkv, n_shares = gridDim.x / p.Hkv, g = blockIdx.x % p.Hkv;      // (heads fastest: 8 heads, one per XCD)
@@ -533,7 +534,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
             };
             const int64_t slot = all.slot(p, share, g);
             if (narrow) {
-                narrow_sums<NW>(sums, p, pc, span, s_all + At::tiles, s_place);
+                narrow_sums<NW>(sums, p, pc, span, s_all + At::tiles, (int*)s_notes);
                 claim();
                 // the waves' sums meet: rows of 32 x 16 bytes per wave, turned by the row (banks)
                 const int n = lane & 31, kh = lane >> 5;
@@ -587,7 +588,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
                 if (pieces > 1 && last_to_arrive(word, p.tag, pieces, &s_flag))
                     for (int row = wave; row < rows; row += NW) merge_row(p, all, row, g, rq.t0 + (row >> p.gs), (g << p.gs) + (row & (p.G - 1)), lane);
             } else {
-                wide_sums<NW, true>(sums, p, pc, span, s_all + At::tiles, &s_odd, s_place);
+                wide_sums<NW, true>(sums, p, pc, span, s_all + At::tiles, &s_odd, s_notes);
                 claim();
                 const int row = pc.row0 + 32 * wave + (lane & 31);
                 const bool active = pc.row0 + 32 * wave < rows;

@@ -30,7 +30,8 @@ namespace span {
 
 constexpr int kRing = 4;                                // tiles of K, and of V, in LDS
 constexpr int kRingBytes = 2 * kRing * kTileBytes;
-constexpr int kTurn = 1024;                             // key tiles whose pages are looked up at a time
+constexpr int kTurn = 512;                              // key tiles that are looked up at a time
+constexpr int kNotes = kTurn + 8;                       // and what lies behind them: see Note
 constexpr float kPMax = 15.f, kLift = 8.f;
 constexpr float kMasked = -INFINITY;                    // a score that takes no part
 
@@ -258,6 +259,15 @@ __device__ __forceinline__ void load_query(half8_t (&tq)[8], const Params& p, co
     for (int s = 0; s < 8; ++s) pin(tq[s]);
 }
 
+// What the loop has to know of a key tile, looked up for a whole turn at once.  Behind the turn's last tile follow copies of it
+// that nobody sees: the loop works on four tiles at a time and asks for the next ones ahead.
+struct Note {
+    int place[2];                                                   // of its 16-key halves, in 16 keys of a head, x 4; bits 0: the context's last tile, 1: no page
+    int edge;                                                       // bit w: some row of wave w does not see some key, kEdgeAny: some row of the workgroup, kHidden: nobody sees any
+    int unused;
+};
+constexpr int kLast = 1, kBad = 2, kEdgeAny = 1 << 8, kHidden = 1 << 9;
+
 // Place in the pools, counted in 16 keys of a head, of the 16 keys of a request from position `at` on; -1 if they lie on no page
 __device__ __forceinline__ int place_of(const Params& p, const int32_t* row_of, int g, int at)
 {
@@ -265,23 +275,22 @@ __device__ __forceinline__ int place_of(const Params& p, const int32_t* row_of, 
     return page >= 0 && page < p.n_pages ? (int)(((page * p.Hkv + g) << (p.shift - 4)) + ((at & ((1 << p.shift) - 1)) >> 4)) : -1;
 }
 
-// Sums of the piece's rows, 32 to a wave, over its key tiles.  s_kv: kRingBytes of LDS; s_odd: a word; s_place (paged): 2 kTurn
-// words.  Every wave of the workgroup takes part; its LDS is free again when all have come back and met at a barrier.
+// Sums of the piece's rows, 32 to a wave, over its key tiles.  s_kv: kRingBytes of LDS; s_odd: a word; notes: kNotes of them.
+// Every wave of the workgroup takes part; its LDS is free again when all have come back and met at a barrier.
 template <int NW, bool kPaged>
-__device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Piece& x, const Span& span, unsigned char* s_kv, int* s_odd, int* s_place)
+__device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Piece& x, const Span& span, unsigned char* s_kv, int* s_odd, Note* notes)
 {
     constexpr int kParts = 8 / NW;                                  // pieces of 1 KB of a tile that a wave moves
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte*)s_kv;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, kh = lane >> 5;
     const int wave = scalar(tid >> 6);                              // so that per-wave conditions are scalar branches
     const Request rq = x.rq;
-    const int rows = rq.n << p.gs, last_row = (x.row0 + 32 * NW < rows ? x.row0 + 32 * NW : rows) - 1;
-    // the wave's rows: positions, and the keys a lane's row sees
+    const int rows = rq.n << p.gs;
+    // first and last row of wave w, or of the workgroup: the last key that the first sees, the last one's position
+    auto sees_to = [&](int row) { const int pos = rq.p0 + (row >> p.gs); return pos < rq.limit ? pos : rq.limit - 1; };
+    auto stands_at = [&](int row) { return rq.p0 + ((row < rows ? row : rows - 1) >> p.gs); };
     const int w_row = x.row0 + 32 * wave;
     const bool active = w_row < rows;
-    const int w_last = w_row + 31 < rows ? w_row + 31 : rows - 1;
-    const int w_lo = rq.p0 + (w_row >> p.gs), w_hi = rq.p0 + (w_last >> p.gs), w_all = w_lo < rq.limit ? w_lo : rq.limit - 1;
-    const int b_lo = rq.p0 + (x.row0 >> p.gs), b_hi = rq.p0 + (last_row >> p.gs), b_all = b_lo < rq.limit ? b_lo : rq.limit - 1;
     const int row = w_row + n < rows ? w_row + n : rows - 1;
     const Sight sight(p, rq.p0 + (row >> p.gs), rq.limit);
 
@@ -294,16 +303,18 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
         const int part = wave * kParts + i, r4 = 4 * part, r4l = r4 < (last_key & ~3) ? r4 : last_key & ~3;
         const uint32_t chunk = ((lane & 15) ^ swz(r4 + (lane >> 4))) << 4;
         const int in = lane >> 4, inl = in < last_key - r4l ? in : last_key - r4l;
-        soff[i] = ((kPaged ? r4 & 15 : r4) + in) * 256 + chunk;
-        soff_last[i] = ((kPaged ? r4l & 15 : r4l) + inl) * 256 + chunk;
+        soff[i] = ((r4 & 15) + in) * 256 + chunk;
+        soff_last[i] = ((r4l & 15) + inl) * 256 + chunk;
     }
     const int half = wave * kParts * 4 >> 4;                        // which 16 keys of a tile this wave moves
     const unsigned char* kbase = (const unsigned char*)(kPaged ? p.k : p.k + (int64_t)(x.b * p.Hkv + x.g) * p.N * kD);
     const unsigned char* vbase = (const unsigned char*)(kPaged ? p.v : p.v + (int64_t)(x.b * p.Hkv + x.g) * p.N * kD);
     const uint32_t to0 = lds0 + wave * (kParts * 1024);
-    auto stage_at = [&](const unsigned char* base, int64_t off, bool last, uint32_t slot) {
+    auto stage = [&](const unsigned char* base, int place, uint32_t slot) __attribute__((always_inline)) {
+        base += (uint64_t)(uint32_t)(place & ~3) << 10;             // x 16 rows x 256 bytes
+        const bool last = place & kLast;
 #pragma unroll
-        for (int i = 0; i < kParts; ++i) load_to_lds16(base + off, last ? soff_last[i] : soff[i], to0 + slot * kTileBytes + 1024 * i);
+        for (int i = 0; i < kParts; ++i) load_to_lds16(base, last ? soff_last[i] : soff[i], to0 + slot * kTileBytes + 1024 * i);
     };
     const Operands at(lds0, lds0 + kRing * kTileBytes, lane);
     half8_t tq[8], pr[2][2];
@@ -312,71 +323,78 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
 
     for (int ua = x.from; ua < x.to; ua += kTurn) {
         const int m = x.to - ua < kTurn ? x.to - ua : kTurn;        // tiles of this turn; i counts them
-        auto tile_of = [&](int i) { return span.tile(ua + (i < m ? i : m - 1)); };
-        uint32_t bad = 0;                                           // two bits a tile, from tile i on: its 16-key halves that lie on no page
-        int page_ahead[2] = {0, 0};                                 // places of the tile that the next step asks for
-        int pv[2] = {0, 0}, pk = 0;                                 // of tiles i + 2, i + 3 (V) and i + 4 (K), the wave's half
+        auto tile_of = [&](int i) { return span.tile(ua + i); };
         __syncthreads();                                            // the turn before has been read
-        if (kPaged) {
-            const int32_t* row_of = p.table + (int64_t)x.r * p.table_cap;
-            for (int k = tid; k < 2 * m; k += NW * 64) {
-                int key = span.tile(ua + (k >> 1)) * 32 + 16 * (k & 1);
+        for (int i = tid; i < m + 8; i += NW * 64) {
+            const int tile = tile_of(i < m ? i : m - 1);
+            Note note;
+            note.edge = i < m ? 0 : kHidden | kEdgeAny | 255;
+            int bad = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                int key = tile * 32 + 16 * j, place;
                 if (key > ((span.keys - 1) & ~15)) key = (span.keys - 1) & ~15;
-                s_place[k] = place_of(p, row_of, x.g, key);
+                place = kPaged ? place_of(p, p.table + (int64_t)x.r * p.table_cap, x.g, key) : key >> 4;
+                bad |= place < 0;
+                note.place[j] = (place < 0 ? kBad : place << 2) | (tile == last_tile ? kLast : 0);
             }
-            __syncthreads();
-        }
-        auto pages_of = [&](int i, int& a, int& c) {
-            const int k = i < m ? i : m - 1;
-            a = s_place[2 * k];
-            c = s_place[2 * k + 1];
-        };
-        auto offset_of = [&](int i, int place) -> int64_t {
-            if (kPaged) return (int64_t)(place > 0 ? place : 0) * (16 * kD * 2);
-            return (int64_t)tile_of(i) * kTileBytes;
-        };
-        auto own_place = [&](int i) { return kPaged ? scalar(s_place[2 * (i < m ? i : m - 1) + half]) : 0; };
-        for (int i = 0; i < 4; ++i) stage_at(kbase, offset_of(i, own_place(i)), tile_of(i) == last_tile, i);
-        for (int i = 0; i < 2; ++i) stage_at(vbase, offset_of(i, own_place(i)), tile_of(i) == last_tile, kRing + i);
-        if (kPaged) {
-            for (int i = 0; i < 5; ++i) {
-                int a, c;
-                pages_of(i, a, c);
-                bad |= (uint32_t)((a < 0 ? 1 : 0) | (c < 0 ? 2 : 0)) << (2 * i);
+            if (bad || !sight.whole(tile, sees_to(x.row0), stands_at(x.row0 + 32 * NW - 1))) {
+                note.edge |= kEdgeAny;
+                for (int w = 0; w < NW; ++w)
+                    if (bad || !sight.whole(tile, sees_to(x.row0 + 32 * w), stands_at(x.row0 + 32 * w + 31))) note.edge |= 1 << w;
             }
-            bad = scalar(bad);
-            pv[0] = own_place(2);
-            pv[1] = own_place(3);
-            pk = own_place(4);
-            pages_of(5, page_ahead[0], page_ahead[1]);
+            note.unused = 0;
+            notes[i] = note;
         }
+        if (tid == 0) *s_odd = 0;
         // the V slot of "tile -1" is multiplied with zero probabilities: it has to be finite
 #pragma unroll
         for (int i = 0; i < kParts; ++i) *(uint4_t*)(s_kv + (2 * kRing - 1) * kTileBytes + (i * NW * 64 + tid) * 16) = uint4_t{0u, 0u, 0u, 0u};
+        wait_all_loads();
+        __syncthreads();
+        auto own_place = [&](int i) { return scalar(notes[i].place[half]); };
+        // two bits a tile, from tile i on: edge of the wave, of the workgroup
+        auto edges = [&](int edge) { return (uint32_t)(edge >> wave & 1) | (uint32_t)(edge & kEdgeAny) >> 7; };
+        uint32_t hist = 0;
+        int pk[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            pk[i] = own_place(i);
+            stage(kbase, pk[i], i);
+        }
+        stage(vbase, pk[0], kRing);
+        stage(vbase, pk[1], kRing + 1);
+        int v_next = pk[2], v_then = pk[3], k_next = own_place(4);  // places of tiles i + 2, i + 3 (V) and i + 4 (K)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) hist |= edges(scalar(notes[i].edge)) << (2 * i);
+        int ahead_place = notes[5].place[half], ahead_edge = notes[5].edge;      // of the tile that the next step asks for
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) pr[1][i][j] = (half_t)0.f;
-        if (tid == 0) *s_odd = 0;
         wait_all_loads();
         __syncthreads();
 
-        // stages for step i and brings the places one tile on
-        auto stage_ahead = [&](int i) __attribute__((always_inline)) {
-            stage_at(kbase, offset_of(i + 4, pk), tile_of(i + 4) == last_tile, i & 3);
-            stage_at(vbase, offset_of(i + 2, pv[0]), tile_of(i + 2) == last_tile, kRing + ((i + 2) & 3));
-            if (kPaged) {
-                const int a = scalar(page_ahead[0]), c = scalar(page_ahead[1]);
-                pv[0] = pv[1];
-                pv[1] = pk;
-                pk = half ? c : a;
-                bad = bad >> 2 | (uint32_t)((a < 0 ? 1 : 0) | (c < 0 ? 2 : 0)) << 8;          // now of tiles i + 1 .. i + 5
-                pages_of(i + 6, page_ahead[0], page_ahead[1]);
-            }
+        // stages for step i and brings the places one tile on; returns tile i's edges
+        auto stage_ahead = [&](int i, int T) __attribute__((always_inline)) {
+            stage(kbase, k_next, T);
+            stage(vbase, v_next, kRing + ((T + 2) & 3));
+            v_next = v_then;
+            v_then = k_next;
+            k_next = scalar(ahead_place);
+            const uint32_t now = hist & 3;
+            hist = hist >> 2 | edges(scalar(ahead_edge)) << 8;
+            ahead_place = notes[i + 6].place[half];
+            ahead_edge = notes[i + 6].edge;
+            return now;
+        };
+        auto seen_of = [&](int i) {
+            const Note note = notes[i];
+            const uint32_t bad = scalar((note.place[0] >> 1 & 1) | (note.place[1] & kBad));
+            return scalar(note.edge) & kHidden ? 0u : sight.of_tile(tile_of(i), bad, kh);
         };
         // A hidden key counts as nothing whatever its V holds, but 0 x inf is NaN: in a tile of which some row of the workgroup does not
         // see some key, V that is not finite is cleared in LDS, by the wave that has staged it, and looked at again after the turn.
-        bool edge = false;                                          // tile i is such a tile
         const uint32_t own = lds0 + (kRing * kTileBytes) + wave * (kParts * 1024) + lane * 16;       // what the lane has staged of a V tile
         auto clear_odd = [&](int slot) __attribute__((always_inline)) {
 #pragma unroll
@@ -398,9 +416,9 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         };
         // waits for the tiles of two steps ago; tile i's V is among them
-        auto land = [&](int slot) __attribute__((always_inline)) {
+        auto land = [&](int slot, uint32_t edge) __attribute__((always_inline)) {
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kParts) : "memory");
-            if (__builtin_expect(edge, 0)) clear_odd(slot);
+            if (__builtin_expect(edge & 2, 0)) clear_odd(slot);
             asm volatile("s_barrier" ::: "memory");
         };
 
@@ -417,11 +435,8 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
         // step i: softmax of tile i (its scores s, slot T), scores y of i + 1, value product of i - 1 with its probabilities before
         auto step = [&](int i, int T, float16_t& s, float16_t& y, half8_t(&now)[2], const half8_t(&before)[2]) __attribute__((always_inline)) {
             const int next = (T + 1) & 3, prev = (T + 3) & 3;
-            const int tile = tile_of(i);
-            const uint32_t bits = i < m ? bad & 3 : 3;
-            edge = bits != 0 || !sight.whole(tile, b_all, b_hi);
-            stage_ahead(i);
-            if (__builtin_expect(bits != 0 || !sight.whole(tile, w_all, w_hi), 0)) mask(s, sight.of_tile(tile, bits, kh));
+            const uint32_t edge = stage_ahead(i, T);
+            if (__builtin_expect(edge & 1, 0)) mask(s, seen_of(i));
             float alpha;
             const bool moves = sums.open(s, p.c1, alpha);
             half8_t ka[8], va[8];
@@ -447,9 +462,8 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
             }
             sums.l += sum[0] + sum[1];
             if (__builtin_expect(moves, 0)) sums.rescale(alpha);
-            land(T);
+            land(T, edge);
         };
-        // whole groups of four: tiles behind the turn's last are hidden from every row
         if (active) {
 #pragma unroll 1
             for (int i = 0; i < m; i += 4) {
@@ -463,24 +477,20 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
         } else {                                                    // a wave without rows stages for the others
 #pragma unroll 1
             for (int i = 0; i < ((m + 3) & ~3); ++i) {
-                edge = i >= m || (bad & 3) != 0 || !sight.whole(tile_of(i), b_all, b_hi);
-                stage_ahead(i);
-                land(i & 3);
+                const uint32_t edge = stage_ahead(i, i & 3);
+                land(i & 3, edge);
             }
         }
         // the cleared values of the turn, to the rows that see them
         if (__builtin_expect(scalar(*s_odd), 0)) {
             for (int i = 0; i < m; ++i) {
-                int a = 0, c = 0;
-                if (kPaged) pages_of(i, a, c);
-                const uint32_t bits = scalar((a < 0 ? 1 : 0) | (c < 0 ? 2 : 0));
-                if (bits == 0 && sight.whole(tile_of(i), b_all, b_hi)) continue;
+                if (!(scalar(notes[i].edge) & kEdgeAny)) continue;
                 wait_all_loads();
                 __syncthreads();
-                stage_at(vbase, offset_of(i, own_place(i)), tile_of(i) == last_tile, kRing);
+                stage(vbase, own_place(i), kRing);
                 wait_all_loads();
                 __syncthreads();
-                if (active) add_odd(sums, at, 0, sight.of_tile(tile_of(i), bits, kh));
+                if (active) add_odd(sums, at, 0, seen_of(i));
             }
         }
         wait_all_loads();                                           // nothing may land in LDS after the turn, or the workgroup's end

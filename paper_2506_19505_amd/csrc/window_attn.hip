@@ -8,10 +8,16 @@ namespace {
 
 using namespace span;
 
-template <int NW>                                       // waves of a workgroup: 8 or 4
+// Matrix instructions bound it where windows are long, coming and going (the query rows, the first tiles, the last ones) where they are
+// short.  Waves of a workgroup: four, so that a CU holds two and one computes while the other comes or goes; 8 and 4 measured, us, 32 heads:
+// 8192 tokens, 8 KV heads, window 1024: 183 and 177 (130 GFLOP, 735 TFLOP/s); 16384, window 4096: 1026 and 993 (969 TFLOP/s); 2 x 1531, 32 KV heads,
+// window 256: 60 and 50; 4096, 32 KV heads, window 128: 67 and 56; 16384, window 16384: 2170 and 2123 (1036 TFLOP/s).
+constexpr int NW = 4;
+
 __global__ __launch_bounds__(NW * 64, 2) void window_attn_kernel(const Params p)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[kRingBytes];
+    __shared__ __attribute__((aligned(16))) Note s_notes[kNotes];
     __shared__ int s_odd;
     const int bgs = gridDim.x / p.q_blocks, bg = blockIdx.x % bgs;              // (heads fastest: 8 heads, one per XCD)
     Piece x;
@@ -26,7 +32,7 @@ __global__ __launch_bounds__(NW * 64, 2) void window_attn_kernel(const Params p)
     x.to = span.n;
     Sums sums;
     sums.clear();
-    wide_sums<NW, false>(sums, p, x, span, s_kv, &s_odd, nullptr);
+    wide_sums<NW, false>(sums, p, x, span, s_kv, &s_odd, s_notes);
     const int lane = threadIdx.x & 63, row = x.row0 + 32 * scalar(threadIdx.x >> 6) + (lane & 31);
     if (row < rows) write_row(p, sums, x.b, row >> p.gs, (x.g << p.gs) + (row & (p.G - 1)), lane >> 5);
 }
@@ -42,12 +48,8 @@ hipError_t launch_prefill_attn_window(const Geom& g, const half_t* q, const half
     p.c1 = scale * kLog2e; p.Hkv = g.Hkv; p.G = g.G; p.gs = log2_of(g.G); p.window = window; p.n_sink = n_sink;
     p.N = (int)N; p.Nq = (int)Nq;
     const int64_t pairs = (int64_t)g.B * g.Hkv, rows = Nq * g.G;
-    const bool wide = (rows + 255) / 256 * pairs >= 384;
-    const int span = wide ? 256 : 128;
-    p.q_blocks = (int)((rows + span - 1) / span);
-    const dim3 grid((unsigned)(p.q_blocks * pairs));
-    if (wide) hipLaunchKernelGGL(window_attn_kernel<8>, grid, dim3(512), 0, st, p);
-    else hipLaunchKernelGGL(window_attn_kernel<4>, grid, dim3(256), 0, st, p);
+    p.q_blocks = (int)((rows + 32 * NW - 1) / (32 * NW));
+    hipLaunchKernelGGL(window_attn_kernel, dim3((unsigned)(p.q_blocks * pairs)), dim3(NW * 64), 0, st, p);
     return hipGetLastError();
 }
 
