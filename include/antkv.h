@@ -322,7 +322,7 @@ int antkv_page_map(int64_t R, const int32_t* held_len, const int32_t* new_len, i
 /*
  * Row t of k and v (fp16 [T][Hkv][D], both with element strides xs_t, xs_h, channel stride 1; 16-byte aligned, strides multiples of
  * 8) goes to slot[t] of the pools.  Rows whose slot is negative or behind the pool are skipped.  Slots of one call are distinct:
- * a slot that is given twice holds pieces of either row.  T == 0 is a no-op.  Errors: EINVAL, EUNSUPPORTED, ELAUNCH.
+ * a slot that is given twice holds pieces of either row.  T * Hkv is at most 2^29.  T == 0 is a no-op.  Errors: EINVAL, EUNSUPPORTED, ELAUNCH.
  */
 int antkv_page_store(const antkv_geom* geom, const void* k, const void* v, int64_t xs_t, int64_t xs_h, int64_t T,
                      const int32_t* slot, void* k_pages, void* v_pages, int64_t n_pages, int32_t page_size, void* stream);
@@ -351,7 +351,7 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
  * Rows of T behind q_start[R] are left as they are.  Keys on pages that are none, and positions behind the table's end, are not
  * seen; a row that sees nothing is zero, with row_max -inf and row_sum 0.  What a row does not see has no influence on it, whatever it
  * holds (pages need not be cleared).  Sums have a fixed order: equal inputs give equal bits.
- * n_pages * Hkv * page_size below 2^32.  The workspace size is a function of Hq, Hkv, R and T; calls that share a workspace must not
+ * T * Hq is at most 2^30, n_pages * Hkv * page_size below 2^32.  The workspace size is a function of Hq, Hkv, R and T; calls that share a workspace must not
  * overlap.  Errors: EINVAL, EUNSUPPORTED, EWORKSPACE, ELAUNCH.
  */
 size_t antkv_page_attn_workspace(const antkv_geom* geom, int64_t T);

@@ -38,6 +38,7 @@ int check_pages(int64_t n_pages, int32_t page_size, Pages& pg)
     pg.shift = __builtin_ctz((unsigned)page_size);
     return ANTKV_OK;
 }
+constexpr int64_t kMostBlocks = (1LL << 24) - 1;        // of 256 threads: a grid has fewer than 2^32 threads
 // a block table of so many entries a row; positions stay below 2^30
 inline bool bad_table(int64_t table_cap, const Pages& pg) { return table_cap < 1 || table_cap > (1LL << 30) >> pg.shift; }
 
@@ -296,7 +297,7 @@ int antkv_prefill_attn_window(const antkv_geom* geom, const void* q, const void*
     const int rc = check_geom(geom, g);
     if (rc) return rc;
     if (N <= 0 || Nq <= 0 || Nq > N || N > 1LL << 30 || window < 1 || n_sink < 0) return ANTKV_EINVAL;
-    if (Nq * g.G > 0x7fffffffLL || (Nq * g.G + 127) / 128 * g.B * g.Hkv > 0x7fffffffLL) return ANTKV_EINVAL;
+    if (Nq * g.G > 0x7fffffffLL || (Nq * g.G + 127) / 128 * g.B * g.Hkv > kMostBlocks) return ANTKV_EINVAL;
     if ((row_max == nullptr) != (row_sum == nullptr)) return ANTKV_EINVAL;
     if (g.B == 0) return ANTKV_OK;
     if (!q || !k || !v || !out) return ANTKV_EINVAL;
@@ -333,7 +334,7 @@ int antkv_page_store(const antkv_geom* geom, const void* k, const void* v, int64
     Pages pg;
     rc = check_pages(n_pages, page_size, pg);
     if (rc) return rc;
-    if (T < 0 || T > 0x7fffffffLL || T * g.Hkv > 0x7fffffffLL) return ANTKV_EINVAL;
+    if (T < 0 || T > (1LL << 29) / g.Hkv) return ANTKV_EINVAL;
     if (T == 0) return ANTKV_OK;
     if (!k || !v || !slot || !k_pages || !v_pages || k_pages == v_pages) return ANTKV_EINVAL;
     if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16)) return ANTKV_EINVAL;
@@ -366,7 +367,7 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
 size_t antkv_page_attn_workspace(const antkv_geom* geom, int64_t T)
 {
     Geom g;
-    if (check_geom(geom, g) || g.B > kMapRequests || T < 1 || T > 0x7fffffffLL / g.Hq || g.B == 0) return 0;
+    if (check_geom(geom, g) || g.B > kMapRequests || T < 1 || T > (1LL << 30) / g.Hq || g.B == 0) return 0;
     return page_attn_workspace_bytes(g, T);
 }
 
@@ -382,7 +383,7 @@ int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t
     rc = check_pages(n_pages, page_size, pg);
     if (rc) return rc;
     if (g.B > kMapRequests) return ANTKV_EUNSUPPORTED;
-    if (T < 0 || T > 0x7fffffffLL / g.Hq || bad_table(table_cap, pg) || window < 0 || window > 1LL << 30 || n_sink < 0) return ANTKV_EINVAL;
+    if (T < 0 || T > (1LL << 30) / g.Hq || bad_table(table_cap, pg) || window < 0 || window > 1LL << 30 || n_sink < 0) return ANTKV_EINVAL;
     if (n_pages * g.Hkv > 0x0fffffffLL / (page_size / 16)) return ANTKV_EINVAL;      // places of 16 rows: below 2^28, 1 TB
     if ((row_max == nullptr) != (row_sum == nullptr) || !(scale > 0.f)) return ANTKV_EINVAL;
     if (T == 0 || g.B == 0) return ANTKV_OK;

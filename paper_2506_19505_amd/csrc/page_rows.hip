@@ -105,7 +105,8 @@ hipError_t launch_page_load(int B, int Hkv, const Pages& pg, const half_t* k_pag
                             const int32_t* ctx_len, int64_t first, int64_t N, half_t* k, half_t* v, int64_t xs_b, int64_t xs_h, int64_t xs_t,
                             hipStream_t st)
 {
-    const int64_t blocks = (N + kSpan - 1) / kSpan;
+    int64_t blocks = (N + kSpan - 1) / kSpan;
+    if (blocks > 1 << 20) blocks = 1 << 20;
     hipLaunchKernelGGL(page_load_kernel, dim3((unsigned)blocks, (unsigned)(B * Hkv)), dim3(kThreads), 0, st, (const uint4_t*)k_pages,
                        (const uint4_t*)v_pages, pg.n, pg.shift, table, table_cap, ctx_len, first, N, Hkv, (uint4_t*)k, (uint4_t*)v, xs_b / 8, xs_h / 8,
                        xs_t / 8);

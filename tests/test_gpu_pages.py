@@ -417,6 +417,79 @@ def test_page_attn_on_two_streams():
     assert all(torch.equal(x.view(torch.int16), want[i].view(torch.int16)) for i in range(2) for x in got[i])
 
 
+def test_pools_of_more_than_32_bits():
+    """Pages whose bytes, and whose elements, lie beyond 2^32: stored, loaded and read as those of a small pool."""
+    Hkv, page, n_pages = 8, 256, 18000                              # 4.7e9 elements to a pool
+    kp, vp = (torch.empty((n_pages, Hkv, page, D), dtype=torch.float16, device="cuda") for _ in "kv")
+    assert kp.numel() > 1 << 32
+    ctx, new, gen = [700, 300], [1, 300], gen_of(21)
+    c = Cache(21, ctx, Hkv, page, extra=0)
+    table = ints([[17999, 9000, 17], [4096, 16500, 8192]])
+    geom, T = antkv.Geometry(2, 4 * Hkv, Hkv, 8), sum(ctx)
+    k, v = (torch.cat(x, dim=1).transpose(0, 1).contiguous() for x in (c.k, c.v))
+    pos = np.concatenate([np.arange(n) for n in ctx])
+    pages = np.concatenate([table[r].cpu().numpy()[np.arange(n) // page] for r, n in enumerate(ctx)])
+    antkv.page_store(geom, k, v, ints(pages * page + pos % page), kp, vp)
+    got_k, got_v = antkv.page_load(geom, kp, vp, table, 700, ctx_len=ints(ctx))
+    for r, n in enumerate(ctx):
+        assert torch.equal(got_k[r, :, :n], c.k[r]) and torch.equal(got_v[r, :, :n], c.v[r])
+    q, starts = randn(gen, sum(new), 4 * Hkv, D), ints([0, 1, 301])
+    small = antkv.page_attn(geom, q, SCALE, starts, ints(ctx), c.table, c.k_pages, c.v_pages)[0]
+    assert torch.equal(antkv.page_attn(geom, q, SCALE, starts, ints(ctx), table, kp, vp)[0].view(torch.int16), small.view(torch.int16))
+
+
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (17000, 40)])
+def test_page_attn_hidden_values_far_apart(window, n_sink):
+    """Values that are not finite, in edge tiles of the first and of later turns of the loop over keys: rows that see them, rows that do not."""
+    c = Cache(31, [34000], 1, 32)
+    rows = 200                                                      # positions 33800 .. 33999
+    for at, x in ((3, "inf"), (39, "nan"), (33850, "-inf"), (33999, "nan")):
+        c.v[0][0, at, at % D] = float(x)
+    if window:
+        c.v[0][0, 16900, 7] = float("inf")                          # behind the left edge of some rows
+    c.fill()
+    check_attn(c, [rows], 2, window, n_sink)
+
+
+def test_page_attn_starts_that_do_not_ascend():
+    """Row numbers that are no request's rows are never followed: what lies between proper starts is right."""
+    c = Cache(41, [100, 60, 90], 2, 16)
+    q, geom = randn(gen_of(41), 20, 8, D), antkv.Geometry(3, 8, 2, 8)
+    want = antkv.page_attn(geom, q, SCALE, ints([0, 5, 5, 5]), ints(c.ctx), c.table, c.k_pages, c.v_pages)[0]
+    for starts in ([0, 5, 3, 3], [0, 5, 900, 10 ** 9], [0, 5, -7, -9]):
+        got = antkv.page_attn(geom, q, SCALE, ints(starts), ints(c.ctx), c.table, c.k_pages, c.v_pages)[0]
+        assert torch.equal(got[:3].view(torch.int16), want[:3].view(torch.int16)), starts
+
+
+def test_a_step_on_another_stream():
+    """Map, store, attention, load and a windowed prompt on a stream of their own, each reading what the one before has written."""
+    Hq, Hkv, page, n_pages, n = 8, 2, 16, 40, 500
+    gen, geom, one = gen_of(51), antkv.Geometry(1, Hq, Hkv, 8), ints([n])
+    k, v, q = randn(gen, n, Hkv, D), randn(gen, n, Hkv, D), randn(gen, n, Hq, D)
+    free = torch.randperm(n_pages, device="cuda", generator=gen).to(torch.int32)
+
+    def step():
+        kp, vp = (torch.zeros((n_pages, Hkv, page, D), dtype=torch.float16, device="cuda") for _ in "kv")
+        table = torch.full((1, n_pages), -1, dtype=torch.int32, device="cuda")
+        ctx, starts, slot, _ = antkv.page_map(ints([0]), one, table, page, n_pages, free, n)
+        antkv.page_store(geom, k, v, slot, kp, vp)
+        out = antkv.page_attn(geom, q, SCALE, starts, ctx, table, kp, vp, window=90, n_sink=3)[0]
+        dk, dv = antkv.page_load(geom, kp, vp, table, n)
+        dense = antkv.prefill_attn_window(geom, q.transpose(0, 1)[None].contiguous(), dk, dv, SCALE, 90, 3, want_stats=False)[0]
+        return out, dk, dv, dense
+
+    want = step()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            got = step()
+    side.synchronize()
+    assert all(torch.equal(g.view(torch.int16), w.view(torch.int16)) for g, w in zip(got, want))
+    a, b = want[0].transpose(0, 1).double(), want[3][0].double()
+    assert ((a - b).norm(dim=-1) <= 2 * OUT_TOL * b.norm(dim=-1)).all()
+
+
 # ------------------------------------------------------------------------------------------------ windowed prompts
 
 @pytest.mark.parametrize("window,n_sink", [(1, 0), (1, 1), (7, 4), (32, 0), (33, 32), (128, 70), (10 ** 9, 10 ** 9)])

@@ -119,3 +119,12 @@ def test_bindings_refuse_host_tensors_and_wrong_shapes():
         antkv.page_attn(geom, half(1, 8, 128), 0.1, ints(2), ints(1), ints(1, 4), *pools)
     with pytest.raises(ValueError):
         antkv.prefill_attn_window(geom, half(1, 8, 4, 128), half(1, 2, 4, 128), half(1, 2, 4, 128), 0.1, 4)
+
+
+def test_batches_beyond_a_grid(lib):
+    one = _g(Hq=8, Hkv=8)
+    assert _store(lib, T=(1 << 28) + 1) == EINVAL
+    assert _attn(lib, T=(1 << 27) + 1) == EINVAL
+    assert lib.antkv_page_attn_workspace(ctypes.byref(_g()), (1 << 27) + 1) == 0 < lib.antkv_page_attn_workspace(ctypes.byref(_g()), 1 << 27)
+    assert _attn(lib, g=one, n_pages=1 << 26) == EINVAL              # (2^33 rows of a head)
+    assert _window(lib, N=1 << 30, Nq=1 << 30) == _window(lib, g=one, N=1 << 30, Nq=1 << 30) == _window(lib, g=one, N=1 << 28, Nq=1 << 28) == EINVAL
