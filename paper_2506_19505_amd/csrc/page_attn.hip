@@ -50,8 +50,7 @@ __device__ __forceinline__ Request request_of(const Params& p, int r)
 
 // ---- the plan --------------------------------------------------------------------------------------------------------------------
 
-// Costs of a request's blocks, last one (the longest) first: a, a - step, a - 2 step, ..  A key tile costs 1 in a narrow block, where
-// it has to come in, and 2 in a wide one, where the waves compute on it (0.55 and 1.2 us where both run side by side).
+// Costs of a request's blocks, last one (the longest) first: a, a - step, a - 2 step, ..
 template <int NW>
 struct Cost {
     static constexpr int kRows = 32 * NW;                           // of a block
@@ -63,15 +62,14 @@ struct Cost {
         a = step = 0;
         if (blocks > 0) {
             const int first = (blocks - 1) * (kRows >> p.gs);
-            a = span_of(q.p0 + first, q.p0 + q.n - 1, q.limit, p.window, p.n_sink).n * tile(rows) + idle(rows);
+            a = span_of(q.p0 + first, q.p0 + q.n - 1, q.limit, p.window, p.n_sink).n + idle(rows);
             // causal: each block sees as many tiles less as it has tokens / 32; not so in a window, or where the table ends early
-            if (p.window == 0 && q.p0 >= 0 && q.p0 + q.n <= q.limit) step = (kRows / 32 >> p.gs) * tile(rows);
+            if (p.window == 0 && q.p0 >= 0 && q.p0 + q.n <= q.limit) step = kRows / 32 >> p.gs;
         }
     }
     // Key tiles' worth of coming and going: looking up pages, the first loads, partial sums.  64 requests of 1 .. 32768 keys, a token each,
     // with 4, 14, 20, 28, 40: 247, 202, 192, 178, 179 us in workgroups of 8 waves, with 10, 20, 28: 187, 181, 180 in workgroups of 4
-    __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? 20 : 32; }
-    __device__ __forceinline__ static int tile(int rows) { return rows <= kNarrow ? 1 : 2; }
+    __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? 20 : 16; }
     __device__ __forceinline__ int before(int k) const { return k * a - step * (k * (k - 1) / 2); }      // of blocks 0 .. k - 1
     __device__ __forceinline__ int all() const { return before(blocks); }
     __device__ __forceinline__ int block_at(int x) const            // the block in which x lies
@@ -458,10 +456,10 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
     // loop over pieces on such values would be run under a mask of lanes.
     cur.unit = scalar(blocks * p.Hkv >= kBlocksEach * (kWaves / NW) || about >= 1e9f) != 0;
     wide = scalar(wide);
-    int size = 1, x = share, end = blocks;                                    // the share: costs x .. end - 1 (unit: blocks x, x + n_shares, ..)
+    int size = 1, x = share, end = blocks;                          // the share: costs x .. end - 1 (unit: blocks x, x + n_shares, ..)
     if (!cur.unit) {
         size = (total + p.shares - 1) / p.shares;
-        const int least = wide ? 96 : 12;
+        const int least = wide ? 48 : 12;
         if (size < least) size = least;
         x = share < p.shares ? share * size : total;
         end = x + size < total ? x + size : total;
@@ -511,11 +509,11 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
         bool some = true;                                           // the piece has tiles, or is the only one
         if (!cur.unit) {
             // cost offset -> tile: what lies behind the idle part, cut at every fourth (wide blocks are worked on four at a time)
-            const int idle = Cost<NW>::idle(rows), four = 4 * Cost<NW>::tile(rows);
-            auto tile_at = [&](int off) { const int t = (off - idle) / four * 4; return t <= 0 ? 0 : off >= len || t > span.n ? span.n : t; };
+            const int idle = Cost<NW>::idle(rows), round = 4;
+            auto tile_at = [&](int off) { const int t = off - idle; return t <= 0 ? 0 : off >= len ? span.n : t / round * round < span.n ? t / round * round : span.n; };
             all.start = c0 >= share * size ? share : c0 / size;
             all.last = c0 + len <= (share + 1) * size ? share : (c0 + len - 1) / size;
-            all.first = (c0 + idle + four - 1) / size;              // the first with a tile
+            all.first = (c0 + idle + round + size - 1) / size - 1;  // the first with a tile
             if (all.first < all.start) all.first = all.start;
             if (all.first > all.last) all.first = all.last;
             some = share >= all.first;
