@@ -343,19 +343,15 @@ __device__ __forceinline__ void merge_row(const Params& p, const Pieces& pc, int
     }
 }
 
-// Wide blocks leave their registers as they are, 64 lanes x 16 bytes at a time.
+// Wide blocks leave their registers as they are, 64 lanes x 8 bytes at a time: whole lines, which is what goes past the caches well.
 __device__ __forceinline__ float* wide_part(const Params& p, int64_t slot, int wave, int i, int lane)
 {
-    return p.part_out + slot * p.rows_cap * kD + ((wave * 16 + i) * 64 + lane) * 4;
+    return p.part_out + slot * p.rows_cap * kD + ((wave * 32 + i) * 64 + lane) * 2;
 }
 __device__ __forceinline__ void store_wide(const Params& p, const Sums& x, int64_t slot, int wave, int lane)
 {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float* to = wide_part(p, slot, wave, i, lane);
-        store_part(to, x.o[i >> 2][4 * (i & 3)], x.o[i >> 2][4 * (i & 3) + 1]);
-        store_part(to + 2, x.o[i >> 2][4 * (i & 3) + 2], x.o[i >> 2][4 * (i & 3) + 3]);
-    }
+    for (int i = 0; i < 32; ++i) store_part(wide_part(p, slot, wave, i, lane), x.o[i >> 3][2 * (i & 7)], x.o[i >> 3][2 * (i & 7) + 1]);
     if (lane < 32) {
         float* stat = p.part_stat + 4 * (slot * p.rows_cap + 32 * wave + lane);
         store_part(stat, x.m_ref, x.l);
@@ -371,21 +367,16 @@ __device__ __forceinline__ void merge_wide(const Params& p, Sums& x, const Piece
         const float2_t u = load_part(stat), v = load_part(stat + 2);
         float2_t o[32];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float* from = wide_part(p, slot, wave, i, lane);
-            o[2 * i] = load_part(from);
-            o[2 * i + 1] = load_part(from + 2);
-        }
+        for (int i = 0; i < 32; ++i) o[i] = load_part(wide_part(p, slot, wave, i, lane));
         const bool some = u[1] != 0.f;                              // (also where it is NaN)
         const float m_new = some ? fmaxf(x.m_ref, u[0]) : x.m_ref, back = fast_exp2(x.m_ref - m_new), w = some ? fast_exp2(u[0] - m_new) : 0.f;
         x.m_ref = m_new;
         x.s_max = fmaxf(x.s_max, v[0]);
         x.l = x.l * back + (some ? u[1] * w : 0.f);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < 32; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                x.o[i >> 2][4 * (i & 3) + e] = fmaf(o[2 * i + (e >> 1)][e & 1], w, x.o[i >> 2][4 * (i & 3) + e] * back);
+            for (int e = 0; e < 2; ++e) x.o[i >> 3][2 * (i & 7) + e] = fmaf(o[i][e], w, x.o[i >> 3][2 * (i & 7) + e] * back);
     }
 }
 
@@ -549,8 +540,8 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
                     if (kh == 0) s_stat[wave * kNarrow + n] = float4_t{sums.m_ref, sums.l, sums.s_max, 0.f};
                 }
                 __syncthreads();
-                for (int u = tid; u < rows * 32; u += kThreads) {
-                    const int row = u >> 5, c4 = u & 31, t = rq.t0 + (row >> p.gs), h = (g << p.gs) + (row & (p.G - 1));
+                for (int u = tid; u < rows * (kD / 2); u += kThreads) {             // two channels to a lane
+                    const int row = u >> 6, c2 = u & 63, t = rq.t0 + (row >> p.gs), h = (g << p.gs) + (row & (p.G - 1));
                     float m = kNegBig, s_max = kMasked, sum = 0.f;
                     float4_t st[NW];
 #pragma unroll
@@ -559,27 +550,26 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
                         if (st[w][1] != 0.f) m = fmaxf(m, st[w][0]);
                         s_max = fmaxf(s_max, st[w][2]);
                     }
-                    float4_t o = {0.f, 0.f, 0.f, 0.f};
+                    float2_t o = {0.f, 0.f};
 #pragma unroll
                     for (int w = 0; w < NW; ++w) {
                         const float f = st[w][1] != 0.f ? fast_exp2(st[w][0] - m) : 0.f;       // (a sum of NaN counts)
                         if (f != 0.f) sum = fmaf(st[w][1], f, sum);
-                        const float4_t v = s_sum[(w * kNarrow + row) * 32 + ((c4 + row) & 31)];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], f, o[e]);
+                        const float2_t v = ((const float2_t*)&s_sum[(w * kNarrow + row) * 32 + (((c2 >> 1) + row) & 31)])[c2 & 1];
+                        o[0] = fmaf(v[0], f, o[0]);
+                        o[1] = fmaf(v[1], f, o[1]);
                     }
                     if (pieces == 1) {
                         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                        *(half4_t*)(p.out + t * p.os_t + h * p.os_h + 4 * c4) = half4_t{(half_t)(o[0] * inv), (half_t)(o[1] * inv), (half_t)(o[2] * inv), (half_t)(o[3] * inv)};
-                        if (c4 == 0 && p.row_max) {
+                        *(half2_t*)(p.out + t * p.os_t + h * p.os_h + 2 * c2) = half2_t{(half_t)(o[0] * inv), (half_t)(o[1] * inv)};
+                        if (c2 == 0 && p.row_max) {
                             p.row_max[h * p.st_h + t] = s_max * p.c1 * (1.f / kLog2e);
                             p.row_sum[h * p.st_h + t] = sum == 0.f ? 0.f : sum * fast_exp2(fmaf(-s_max, p.c1, m));
                         }
                     } else {
                         const int64_t at = slot * p.rows_cap + row;
-                        store_part(p.part_out + at * kD + 4 * c4, o[0], o[1]);
-                        store_part(p.part_out + at * kD + 4 * c4 + 2, o[2], o[3]);
-                        if (c4 == 0) {
+                        store_part(p.part_out + at * kD + 2 * c2, o[0], o[1]);
+                        if (c2 == 0) {
                             store_part(p.part_stat + 4 * at, m, sum);
                             store_part(p.part_stat + 4 * at + 2, s_max, 0.f);
                         }
