@@ -358,26 +358,33 @@ __device__ __forceinline__ void store_wide(const Params& p, const Sums& x, int64
         store_part(stat + 2, x.s_max, 0.f);
     }
 }
-__device__ __forceinline__ void merge_wide(const Params& p, Sums& x, const Pieces& pc, int g, int wave, int lane)
+__device__ __forceinline__ void merge_wide(const Params& p, Sums& x, const Pieces& pc, int share, int g, int wave, int lane)
 {
-    x.clear();
+    Sums all;
+    all.clear();
     for (int s = pc.first; s <= pc.last; ++s) {                     // always in the order of the keys
-        const int64_t slot = pc.slot(p, s, g);
-        const float* stat = p.part_stat + 4 * (slot * p.rows_cap + 32 * wave + (lane & 31));
-        const float2_t u = load_part(stat), v = load_part(stat + 2);
-        float2_t o[32];
+        float2_t u = {x.m_ref, x.l}, v = {x.s_max, 0.f}, o[32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = load_part(wide_part(p, slot, wave, i, lane));
+        for (int i = 0; i < 32; ++i) o[i] = float2_t{x.o[i >> 3][2 * (i & 7)], x.o[i >> 3][2 * (i & 7) + 1]};
+        if (s != share) {                                           // (its own are in registers still)
+            const int64_t slot = pc.slot(p, s, g);
+            const float* stat = p.part_stat + 4 * (slot * p.rows_cap + 32 * wave + (lane & 31));
+            u = load_part(stat);
+            v = load_part(stat + 2);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = load_part(wide_part(p, slot, wave, i, lane));
+        }
         const bool some = u[1] != 0.f;                              // (also where it is NaN)
-        const float m_new = some ? fmaxf(x.m_ref, u[0]) : x.m_ref, back = fast_exp2(x.m_ref - m_new), w = some ? fast_exp2(u[0] - m_new) : 0.f;
-        x.m_ref = m_new;
-        x.s_max = fmaxf(x.s_max, v[0]);
-        x.l = x.l * back + (some ? u[1] * w : 0.f);
+        const float m_new = some ? fmaxf(all.m_ref, u[0]) : all.m_ref, back = fast_exp2(all.m_ref - m_new), w = some ? fast_exp2(u[0] - m_new) : 0.f;
+        all.m_ref = m_new;
+        all.s_max = fmaxf(all.s_max, v[0]);
+        all.l = all.l * back + (some ? u[1] * w : 0.f);
 #pragma unroll
         for (int i = 0; i < 32; ++i)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) x.o[i >> 3][2 * (i & 7) + e] = fmaf(o[i][e], w, x.o[i >> 3][2 * (i & 7) + e] * back);
+            for (int e = 0; e < 2; ++e) all.o[i >> 3][2 * (i & 7) + e] = fmaf(o[i][e], w, all.o[i >> 3][2 * (i & 7) + e] * back);
     }
+    x = all;
 }
 
 // ---- the kernel ------------------------------------------------------------------------------------------------------------------
@@ -586,7 +593,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
                 if (pieces > 1) {
                     if (active) store_wide(p, sums, slot, wave, lane);
                     mine = last_to_arrive(word, p.tag, pieces, &s_flag);
-                    if (mine && active) merge_wide(p, sums, all, g, wave, lane);
+                    if (mine && active) merge_wide(p, sums, all, share, g, wave, lane);
                 }
                 if (mine && row < rows) write_row(p, sums, 0, rq.t0 + (row >> p.gs), (g << p.gs) + (row & (p.G - 1)), lane >> 5);
             }
