@@ -344,7 +344,7 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
  * with j > position - window or j < n_sink (window 0: no limit, at most 2^30).  Any mix of requests with no, one or thousands of rows.
  *
  *   q        fp16 [T][Hq][D] with element strides qs_t, qs_h (multiples of 8), 16-byte aligned
- *   q_start  int32 [R + 1] ascending from 0;  ctx_len int32 [R];  table as above
+ *   q_start  int32 [R + 1] ascending from 0 (otherwise rows between its entries may stay as they are);  ctx_len int32 [R];  table as above
  *   out      fp16 [T][Hq][D]; accumulation is fp32, rounded once; probabilities enter the value product rounded to fp16
  *   row_max, row_sum  optional fp32 [Hq][T] (both or neither) as antkv_prefill_attn's: for a single request the layout that
  *            antkv_anchor_select takes with Nq = T

@@ -5,7 +5,7 @@
 // and going.  Laid end to end, the costs of all blocks are cut into equal shares, one for each of the workgroups that the chip holds at a
 // time (the KV heads on their own XCDs), wherever the cuts fall: the middle of a long context, or behind a few short
 // ones.  Every workgroup derives the same cuts from the requests' lengths.  A block that is cut leaves partial sums, which the
-// last of its workgroups to end adds up.  With many blocks (kBlocksEach to a workgroup) each is a workgroup of its own instead.
+// last of its workgroups to end adds up.  Long prompts in one go are many long blocks: each is a workgroup of its own (Params::unit).
 //
 // Wide blocks, of more than 32 rows: the waves have 32 rows each and share the key tiles (wide_sums).
 // Narrow blocks (a token or a few of a request): there is one tile of rows, and memory is what bounds it.  Every wave streams key tiles
@@ -25,7 +25,6 @@ constexpr int kNarrow = 32;
 constexpr int kTurnNarrow = 1024;                                   // key tiles of a narrow block whose pages are looked up at a time
 constexpr int kWindow = 64;                                         // requests that a wave looks at at a time
 constexpr int kWindows = kMapRequests / kWindow;
-constexpr int kBlocksEach = 4;
 constexpr int kWaves = 2048;                                        // that the chip holds at a time: two to a SIMD
 
 template <int NW>                                       // waves of a workgroup: 8 or 4
@@ -67,8 +66,8 @@ struct Cost {
             if (p.window == 0 && q.p0 >= 0 && q.p0 + q.n <= q.limit) step = kRows / 32 >> p.gs;
         }
     }
-    // Key tiles' worth of coming and going: looking up pages, the first loads, partial sums.  64 requests of 1 .. 32768 keys, a token each,
-    // with 4, 14, 20, 28, 40: 247, 202, 192, 178, 179 us in workgroups of 8 waves, with 10, 20, 28: 187, 181, 180 in workgroups of 4
+    // Key tiles' worth of coming and going: looking up pages, the first loads, partial sums.  64 requests of a token on 1 .. 32768 keys with
+    // 4, 20, 28: 208, 176, 178 us; 16 requests, some with hundreds of tokens, with 10, 12, 16, 20 for their wide blocks: 92, 87.5, 87.6, 89
     __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? 20 : 16; }
     __device__ __forceinline__ int before(int k) const { return k * a - step * (k * (k - 1) / 2); }      // of blocks 0 .. k - 1
     __device__ __forceinline__ int all() const { return before(blocks); }
@@ -108,18 +107,12 @@ struct Cursor {
     Request q;                                                      // the lane's request
     int upto;                                                       // and the costs up to its end, from the window's start on
     int window, base;                                               // first request / 64, costs before it
-    bool unit;                                                      // every block costs 1
-
-    __device__ __forceinline__ int cost(const Params& p, const Request& u) const
-    {
-        const Cost<NW> c(p, u);
-        return unit ? c.blocks : c.all();
-    }
     __device__ __forceinline__ void look(const Params& p)
     {
         const int r = window * kWindow + (threadIdx.x & 63);
         q = r < p.R ? request_of(p, r) : Request{0, 0, 0, 0};
-        upto = wave_scan(cost(p, q));
+        const Cost<NW> c(p, q);
+        upto = wave_scan(p.unit ? c.blocks : c.all());              // (unit: every block costs 1)
     }
 };
 
@@ -395,80 +388,66 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
     constexpr int kThreads = NW * 64, kRows = 32 * NW;
     using At = Lds<NW>;
     __shared__ __attribute__((aligned(1024))) unsigned char s_all[At::total];
-    __shared__ int s_cost[kWindows], s_blocks[kWindows], s_odd, s_flag;
+    __shared__ int s_cost[kWindows], s_odd, s_flag;
+    __shared__ float s_tokens;
     Note* s_notes = (Note*)(s_all + At::notes);
     float4_t* s_stat = (float4_t*)(s_all + At::stat);
     const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6);
-    const int share = blockIdx.x / p.Hkv, n_shares = gridDim.x / p.Hkv, g = blockIdx.x % p.Hkv;      // (heads fastest: 8 heads, one per XCD)
+    const int share = blockIdx.x / p.Hkv, g = blockIdx.x % p.Hkv;      // (heads fastest: 8 heads, one per XCD)
 
     // the costs of all requests
     Cursor<NW> cur;
     cur.window = cur.base = 0;
-    cur.unit = false;
     const int windows = (p.R + kWindow - 1) / kWindow;
-    int total = 0, blocks = 0, wide = 0;
-    float about = 0.f;                                              // the total, where it does not fit an int
-    {
-        auto tally = [&](int& cost, int& some, bool& any_wide, float& f) {
-            const Cost<NW> c(p, cur.q);
-            some = last_lane(wave_scan(c.blocks));
-            cost = last_lane(cur.upto);
-            any_wide = __any((cur.q.n << p.gs) > kNarrow);
-            f = wave_sum((float)c.blocks * (float)c.a);
-        };
-        if (windows == 1) {
-            bool any;
-            cur.look(p);
-            tally(total, blocks, any, about);
-            wide = any;
-        } else {
-            if (tid == 0) s_flag = 0;
-            __syncthreads();
-            for (int w = wave; w < windows; w += NW) {
-                int cost, some;
-                bool any;
-                float f;
-                cur.window = w;
-                cur.look(p);
-                tally(cost, some, any, f);
-                if (lane == 0) {
-                    s_cost[w] = f < 1e8f ? cost : -1;
-                    s_blocks[w] = some;
-                    if (any) s_flag = 1;
-                }
-            }
-            __syncthreads();
-            wide = scalar(s_flag);
-            for (int w = 0; w < windows; ++w) {
-                const int c = scalar(s_cost[w]);
-                total += c < 0 ? 0 : c;
-                blocks += scalar(s_blocks[w]);
-                about += c < 0 ? 1e9f : (float)c;
-            }
-            cur.window = -1;
+    int total = 0, wide = 0;
+    float tokens;                                                   // of all requests: more than the batch has only if they overlap
+    if (windows == 1) {
+        cur.look(p);
+        total = last_lane(cur.upto);
+        tokens = wave_sum((float)cur.q.n);
+        wide = __any((cur.q.n << p.gs) > kNarrow);
+    } else {
+        if (tid == 0) {
+            s_flag = 0;
+            s_tokens = 0.f;
         }
+        __syncthreads();
+        for (int w = wave; w < windows; w += NW) {
+            cur.window = w;
+            cur.look(p);
+            const int cost = last_lane(cur.upto);
+            const float some = wave_sum((float)cur.q.n);
+            const bool any = __any((cur.q.n << p.gs) > kNarrow);
+            if (lane == 0) {
+                s_cost[w] = cost;
+                atomicAdd(&s_tokens, some);
+                if (any) s_flag = 1;
+            }
+        }
+        __syncthreads();
+        wide = s_flag;
+        tokens = s_tokens;
+        for (int w = 0; w < windows; ++w) total += scalar(s_cost[w]);
     }
-    total = scalar(total);
-    blocks = scalar(blocks);
     // All of the plan is the same in every lane, and has to be so to the compiler too: values that come out of a shuffle are not, and a
     // loop over pieces on such values would be run under a mask of lanes.
-    cur.unit = scalar(blocks * p.Hkv >= kBlocksEach * (kWaves / NW) || about >= 1e9f) != 0;
+    total = scalar(total);
     wide = scalar(wide);
-    int size = 1, x = share, end = blocks;                          // the share: costs x .. end - 1 (unit: blocks x, x + n_shares, ..)
-    if (!cur.unit) {
+    if (scalar(tokens > 1.01f * (float)p.T)) return;                // costs that might not fit
+    int size = 1, x = share, end = total;                           // the share: costs x .. end - 1 (unit: block x)
+    if (!p.unit) {
         size = (total + p.shares - 1) / p.shares;
-        const int least = wide ? 48 : 12;
+        // Less is not worth the partial sums.  4, 12, 24: a token on 4096 keys 20.8, 16.3, 17.3 us; 16, 24, 48, 96: 64 tokens on 4096 keys 35,
+        // 36, 44, 68, 300 on 2000 44, 42, 59, 93, 4 x 100 on 1000 36, 34, 43, 56
+        const int least = wide ? 24 : 12;
         if (size < least) size = least;
         x = share < p.shares ? share * size : total;
         end = x + size < total ? x + size : total;
     }
     if (x >= end) return;
-    if (windows == 1) {
-        if (cur.unit) cur.look(p);
-    } else {                                                        // the window of requests in which the share begins
-        const int* sums = cur.unit ? s_blocks : s_cost;
+    if (windows > 1) {                                              // the window of requests in which the share begins
         int w = 0, before = 0;
-        for (int c = scalar(sums[0]); w + 1 < windows && x >= before + c; c = scalar(sums[w])) {
+        for (int c = scalar(s_cost[0]); w + 1 < windows && x >= before + c; c = scalar(s_cost[w])) {
             before += c;
             ++w;
         }
@@ -494,9 +473,9 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
         const Request rq = pc.rq;
         const Cost<NW> cost(p, rq);
         const int rows = rq.n << p.gs;
-        const int begin = cur.base + __builtin_amdgcn_readlane(cur.upto, l) - (cur.unit ? cost.blocks : cost.all());      // of the request
-        const int k = scalar(cur.unit ? x - begin : cost.block_at(x - begin));
-        const int c0 = begin + (cur.unit ? k : cost.before(k)), len = cur.unit ? 1 : cost.a - cost.step * k;              // of the block
+        const int begin = cur.base + __builtin_amdgcn_readlane(cur.upto, l) - (p.unit ? cost.blocks : cost.all());      // of the request
+        const int k = scalar(p.unit ? x - begin : cost.block_at(x - begin));
+        const int c0 = begin + (p.unit ? k : cost.before(k)), len = p.unit ? 1 : cost.a - cost.step * k;              // of the block
         pc.row0 = (cost.blocks - 1 - k) * kRows;
         const bool narrow = rows <= kNarrow;
         const int last_row = (pc.row0 + kRows < rows ? pc.row0 + kRows : rows) - 1;
@@ -505,7 +484,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
         pc.to = span.n;
         Pieces all = {share, share, share};
         bool some = true;                                           // the piece has tiles, or is the only one
-        if (!cur.unit) {
+        if (!p.unit) {
             // cost offset -> tile: what lies behind the idle part, cut at every fourth (wide blocks are worked on four at a time)
             const int idle = Cost<NW>::idle(rows), round = 4;
             auto tile_at = [&](int off) { const int t = off - idle; return t <= 0 ? 0 : off >= len ? span.n : t / round * round < span.n ? t / round * round : span.n; };
@@ -599,21 +578,30 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
             }
             __syncthreads();                                        // LDS is free for the next piece
         }
-        x = cur.unit ? x + n_shares : c0 + len;
-        if (x >= end) return;
+        x = c0 + len;
+        if (p.unit || x >= end) return;
     }
 }
 
 }  // namespace
 
 // Few long chunks: 8 waves read a key tile for 256 rows; many requests: 4 waves, two workgroups to a CU, one works while the other comes
-// or goes.  8 and 4 waves: a chunk of 2048 on 32768 keys 1.11 and 1.20 ms, 16 requests with 2048 tokens among them (500 for four of
-// them, one for the others) on up to 8192 keys 112 and 94 us, 64 requests of a token each on up to 32768 keys 178 and 180, one on 4096 16.8 and 15.7.
+// or goes.  8 and 4 waves: a chunk of 2048 on 32768 keys 1.00 and 1.11 ms, one of 300 on 2000 42 and 44 us, 8 prompts of 1024 131 and 139, 4 of 100 on 1000 38 and 35, 16 requests with 2048 tokens among them (500 for four of
+// them, one for the others) on up to 8192 keys 97 and 88 us, 64 requests of a token each on up to 32768 keys 182 and 176, one on 4096 17.6 and 16.2.
 static int waves_of(const Geom& g, int64_t T) { return T * g.G >= (int64_t)g.B * 1024 ? 8 : 4; }
 // Shares per KV head: the chip's workgroups, or one each.
 static int shares_of(const Geom& g, int nw) { return g.Hkv < kWaves / nw ? kWaves / nw / g.Hkv : 1; }
 // A batch has no block of more rows than it has itself.
 static int rows_cap_of(const Geom& g, int64_t T, int nw) { return T * g.G < 32 * nw ? ((int)(T * g.G) + 31) / 32 * 32 : 32 * nw; }
+
+// A workgroup per block, where prompts are long and blocks two to a workgroup at least, so that nothing has to be cut: blocks of a prompt
+// that run at the same time are then on about the same keys, which come out of the L2.  In shares and in blocks, 32 heads, 8 KV heads: 16384
+// tokens 2190 and 2157 us, 8192 on 32768 keys 3790 and 3648, 4 x 4096 647 and 627, 8 x 2048 394 and 385, but 8 x 1024 131 and 142, 1000 x 100
+// 886 and 1349, 512 x 1 on 1024 keys 402 and 481.  Also where the costs of all blocks might not fit an int.
+static bool unit_blocks(const Geom& g, int64_t T, int64_t most, int64_t longest)
+{
+    return (T >= 2048 * (int64_t)g.B && T * g.G / 256 * g.Hkv >= 2 * kWaves / 8) || most > (1LL << 30) / (longest / 32 + 32);
+}
 
 // What either would need: a workspace made for many tokens then does for fewer.
 size_t page_attn_workspace_bytes(const Geom& g, int64_t T)
@@ -637,10 +625,9 @@ static hipError_t launch_t(const Geom& g, Params& p, int64_t T, void* ws, hipStr
     p.done = (unsigned long long*)ws;
     p.part_out = (float*)((char*)ws + align_up((size_t)pairs * sizeof(unsigned long long)));
     p.part_stat = p.part_out + 2 * pairs * p.rows_cap * kD;
-    // a workgroup per share, or, if there can be so many, per block
-    const int64_t most = T * g.G / (32 * NW) + (g.B < T ? g.B : T);
-    const int64_t grid = most * g.Hkv >= kBlocksEach * (kWaves / NW) && most > p.shares ? most : p.shares;
-    hipLaunchKernelGGL(page_attn_kernel<NW>, dim3((unsigned)(grid * g.Hkv)), dim3(NW * 64), 0, st, p);
+    const int64_t most = T * g.G / (32 * NW) + (g.B < T ? g.B : T);         // blocks that there can be
+    p.unit = unit_blocks(g, T, most, p.table_cap << p.shift);
+    hipLaunchKernelGGL(page_attn_kernel<NW>, dim3((unsigned)((p.unit ? most : p.shares) * g.Hkv)), dim3(NW * 64), 0, st, p);
     return hipGetLastError();
 }
 

@@ -50,6 +50,7 @@ struct Params {
     int64_t table_cap, n_pages;
     int T, R, shift;
     int shares, rows_cap;                                           // shares of the work per KV head; rows of a piece's partial sums
+    int unit;                                                       // a workgroup per block instead of per share
     unsigned long long* done;                                       // [shares][Hkv] arrival words (launch_tag.h) of the blocks that end there
     uint64_t tag;
     float *part_out, *part_stat;                                    // [2 shares][Hkv][rows_cap] x D sums, x 4: reference, sum, largest score

@@ -461,6 +461,30 @@ def test_page_attn_starts_that_do_not_ascend():
         assert torch.equal(got[:3].view(torch.int16), want[:3].view(torch.int16)), starts
 
 
+def test_page_attn_requests_that_overlap_write_nothing():
+    c, R = Cache(42, [50] * 100, 2, 16), 100
+    q, out = randn(gen_of(42), 30, 8, D), torch.full((30, 8, D), 7.0, dtype=torch.float16, device="cuda")
+    for r in (100, 60):
+        antkv.page_attn(antkv.Geometry(r, 8, 2, 8), q, SCALE, ints([0, 30] * (r // 2) + [0]), ints(c.ctx[:r]), c.table[:r], c.k_pages, c.v_pages, out=out)
+        assert (out == 7.0).all()
+
+
+def test_page_attn_long_prompts():
+    """Blocks enough for a workgroup each: prompts of one length, and one beside a short one, in a window and without."""
+    for window, n_sink in ((0, 0), (300, 40)):
+        check_attn(Cache(51, [4100, 4097], 8, 32), [4100, 4093], 32, window, n_sink, pad=5, each=11)
+        check_attn(Cache(52, [9000, 30], 8, 64), [8800, 2], 32, window, n_sink, each=11)
+
+
+def test_page_attn_tables_of_great_capacity():
+    """Tables for so many tokens that a batch might cost more than the shares can count."""
+    c = Cache(53, [3000, 1, 700] + [20] * 37, 2, 256)
+    table = torch.full((40, 1 << 22), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.table.shape[1]] = c.table
+    c.table = table
+    check_attn(c, [1, 1, 90] + [1] * 37, 8)
+
+
 def test_a_step_on_another_stream():
     """Map, store, attention, load and a windowed prompt on a stream of their own, each reading what the one before has written."""
     Hq, Hkv, page, n_pages, n = 8, 2, 16, 40, 500
