@@ -476,6 +476,15 @@ def test_page_attn_long_prompts():
         check_attn(Cache(52, [9000, 30], 8, 64), [8800, 2], 32, window, n_sink, each=11)
 
 
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (90, 40)])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (4, 2), (3, 3)])
+def test_page_attn_a_token_each_on_average(Hq, Hkv, window, n_sink):
+    """No more rows than requests, but uneven ones: some have many blocks of 32 rows, some none."""
+    ctx = [600, 1, 70, 2000, 33, 64] + [5] * 94
+    check_attn(Cache(61, ctx, Hkv, 32), [40, 1, 0, 33, 17, 0] + [0] * 90 + [5, 0, 1, 1], Hq, window, n_sink, pad=2)
+    check_attn(Cache(62, [3000] + [9] * 129, Hkv, 16), [130] + [0] * 129, Hq, window, n_sink)
+
+
 def test_page_attn_tables_of_great_capacity():
     """Tables for so many tokens that a batch might cost more than the shares can count."""
     c = Cache(53, [3000, 1, 700] + [20] * 37, 2, 256)
