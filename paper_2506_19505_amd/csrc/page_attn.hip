@@ -126,7 +126,7 @@ struct Cursor {
 template <int NW>
 __device__ __forceinline__ void narrow_sums(Sums& sums, const Params& p, const Piece& x, const Span& span, unsigned char* s_tiles, int* s_place)
 {
-    const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, kh = lane >> 5, wave = scalar(tid >> 6);
+    const int tid = own_thread(), lane = tid & 63, n = lane & 31, kh = lane >> 5, wave = scalar(tid >> 6);
     const uint32_t k_at = (uint32_t)(uintptr_t)(lds_byte*)s_tiles + wave * (2 * kTileBytes), v_at = k_at + kTileBytes;
     const Request rq = x.rq;
     const int rows = rq.n << p.gs, row = x.row0 + n < rows ? x.row0 + n : rows - 1;
@@ -462,6 +462,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
     }
 
     for (;;) {
+        const int tid = own_thread(), lane = tid & 63, wave = scalar(tid >> 6);
         // the request in which x lies, its block, the block's pieces
         while (x >= cur.base + last_lane(cur.upto)) {
             if (cur.window + 1 >= windows) return;

@@ -57,6 +57,14 @@ struct Params {
 };
 
 __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }      // of a value that is the same in every lane
+// threadIdx.x, not known to be the same from one piece to the next: what a piece makes of it stays in the piece, where the compiler would
+// take it out of the loop over pieces and, all at once being too much, put it on the stack
+__device__ __forceinline__ int own_thread()
+{
+    int t = threadIdx.x;
+    pin(t);
+    return t;
+}
 __device__ __forceinline__ float max3f(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
 // Key tiles that rows at positions lo .. hi of a context see: tiles 0 .. sink_tiles - 1, then from sink_tiles + gap on.
@@ -283,7 +291,7 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
 {
     constexpr int kParts = 8 / NW;                                  // pieces of 1 KB of a tile that a wave moves
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte*)s_kv;
-    const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, kh = lane >> 5;
+    const int tid = own_thread(), lane = tid & 63, n = lane & 31, kh = lane >> 5;
     const int wave = scalar(tid >> 6);                              // so that per-wave conditions are scalar branches
     const Request rq = x.rq;
     const int rows = rq.n << p.gs;
