@@ -31,11 +31,11 @@ constexpr int kWindow = 64;                                         // requests 
 constexpr int kWindows = kMapRequests / kWindow;
 constexpr int kWaves = 2048;                                        // that the chip holds at a time: two to a SIMD
 
-template <int NW, bool kWide>                           // waves of a workgroup: 8 or 4; whether blocks have up to 32 x NW rows, or 32
+template <int NW>                                       // waves of a workgroup: 8 or 4
 struct Lds {
     static constexpr int tiles = 0;                                 // narrow: a K and a V tile per wave; wide: the rings
     static constexpr int notes = NW * 2 * kTileBytes;               // what is known of the turn's key tiles; narrow: [kTurnNarrow][2] places
-    static constexpr int stat = notes + (kWide ? kNotes * (int)sizeof(Note) : kTurnNarrow * 8);     // [NW][kNarrow][4]: reference, sum, largest score
+    static constexpr int stat = notes + kNotes * (int)sizeof(Note); // [NW][kNarrow][4]: reference, sum, largest score
     static constexpr int total = stat + NW * kNarrow * 16;
     static_assert(kRingBytes <= notes && kTurnNarrow * 8 <= stat - notes && (total + kWindows * 8 + 1024) * (8 / NW) <= 163840, "LDS of a CU");
 };
@@ -54,9 +54,9 @@ __device__ __forceinline__ Request request_of(const Params& p, int r)
 // ---- the plan --------------------------------------------------------------------------------------------------------------------
 
 // Costs of a request's blocks, last one (the longest) first: a, a - step, a - 2 step, ..
-template <int NW, bool kWide>
+template <int NW>
 struct Cost {
-    static constexpr int kRows = kWide ? 32 * NW : kNarrow;         // of a block
+    static constexpr int kRows = 32 * NW;                           // of a block
     int blocks, a, step;
     __device__ __forceinline__ Cost(const Params& p, const Request& q)
     {
@@ -72,7 +72,7 @@ struct Cost {
     }
     // Key tiles' worth of coming and going: looking up pages, the first loads, partial sums.  64 requests of a token on 1 .. 32768 keys with
     // 4, 20, 28: 208, 176, 178 us; 16 requests, some with hundreds of tokens, with 10, 12, 16, 20 for their wide blocks: 92, 87.5, 87.6, 89
-    __device__ __forceinline__ static int idle(int rows) { return !kWide || rows <= kNarrow ? 20 : 16; }
+    __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? 20 : 16; }
     __device__ __forceinline__ int before(int k) const { return k * a - step * (k * (k - 1) / 2); }      // of blocks 0 .. k - 1
     __device__ __forceinline__ int all() const { return before(blocks); }
     __device__ __forceinline__ int block_at(int x) const            // the block in which x lies
@@ -106,7 +106,7 @@ __device__ __forceinline__ int wave_scan(int x)
 __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
 // Where a workgroup is in the laid-out blocks: 64 requests at a time, one to a lane.  All other members are the same in every lane.
-template <int NW, bool kWide>
+template <int NW>
 struct Cursor {
     Request q;                                                      // the lane's request
     int upto;                                                       // and the costs up to its end, from the window's start on
@@ -115,7 +115,7 @@ struct Cursor {
     {
         const int r = window * kWindow + (threadIdx.x & 63);
         q = r < p.R ? request_of(p, r) : Request{0, 0, 0, 0};
-        const Cost<NW, kWide> c(p, q);
+        const Cost<NW> c(p, q);
         upto = wave_scan(p.unit ? c.blocks : c.all());              // (unit: every block costs 1)
     }
 };
@@ -129,9 +129,8 @@ __device__ __forceinline__ void narrow_sums(Sums& sums, const Params& p, const P
     const int tid = own_thread(), lane = tid & 63, n = lane & 31, kh = lane >> 5, wave = scalar(tid >> 6);
     const uint32_t k_at = (uint32_t)(uintptr_t)(lds_byte*)s_tiles + wave * (2 * kTileBytes), v_at = k_at + kTileBytes;
     const Request rq = x.rq;
-    const int rows = rq.n << p.gs, row = x.row0 + n < rows ? x.row0 + n : rows - 1;
-    const int lo = rq.p0 + (x.row0 >> p.gs), hi = rq.p0 + ((x.row0 + kNarrow < rows ? x.row0 + kNarrow : rows) - 1 >> p.gs);
-    const int all = lo < rq.limit ? lo : rq.limit - 1;
+    const int rows = rq.n << p.gs, row = n < rows ? n : rows - 1;
+    const int hi = rq.p0 + rq.n - 1, all = rq.p0 < rq.limit ? rq.p0 : rq.limit - 1;
     const Sight sight(p, rq.p0 + (row >> p.gs), rq.limit);
     const int last_tile = (span.keys - 1) >> 5, last_key = (span.keys - 1) & 31;
     // staging: 1 KB, four rows, per load; rows behind the last key repeat it
@@ -387,11 +386,11 @@ __device__ __forceinline__ void merge_wide(const Params& p, Sums& x, const Piece
 
 // ---- the kernel ------------------------------------------------------------------------------------------------------------------
 
-template <int NW, bool kWide>
+template <int NW>
 __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
 {
-    constexpr int kThreads = NW * 64, kRows = Cost<NW, kWide>::kRows;
-    using At = Lds<NW, kWide>;
+    constexpr int kThreads = NW * 64, kRows = 32 * NW;
+    using At = Lds<NW>;
     __shared__ __attribute__((aligned(1024))) unsigned char s_all[At::total];
     __shared__ int s_cost[kWindows], s_odd, s_flag;
     __shared__ float s_tokens;
@@ -401,7 +400,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
     const int share = blockIdx.x / p.Hkv, g = blockIdx.x % p.Hkv;      // (heads fastest: 8 heads, one per XCD)
 
     // the costs of all requests
-    Cursor<NW, kWide> cur;
+    Cursor<NW> cur;
     cur.window = cur.base = 0;
     const int windows = (p.R + kWindow - 1) / kWindow;
     int total = 0, wide = 0;
@@ -444,7 +443,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
         size = (total + p.shares - 1) / p.shares;
         // Less is not worth the partial sums.  4, 12, 24: a token on 4096 keys 20.8, 16.3, 17.3 us; 16, 24, 48, 96: 64 tokens on 4096 keys 35,
         // 36, 44, 68, 300 on 2000 44, 42, 59, 93, 4 x 100 on 1000 36, 34, 43, 56
-        const int least = kWide && wide ? 24 : 12;
+        const int least = wide ? 24 : 12;
         if (size < least) size = least;
         x = share < p.shares ? share * size : total;
         end = x + size < total ? x + size : total;
@@ -477,13 +476,13 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
         pc.r = cur.window * kWindow + l;
         pc.rq = {__builtin_amdgcn_readlane(cur.q.t0, l), __builtin_amdgcn_readlane(cur.q.n, l), __builtin_amdgcn_readlane(cur.q.p0, l), __builtin_amdgcn_readlane(cur.q.limit, l)};
         const Request rq = pc.rq;
-        const Cost<NW, kWide> cost(p, rq);
+        const Cost<NW> cost(p, rq);
         const int rows = rq.n << p.gs;
         const int begin = cur.base + __builtin_amdgcn_readlane(cur.upto, l) - (p.unit ? cost.blocks : cost.all());      // of the request
         const int k = scalar(p.unit ? x - begin : cost.block_at(x - begin));
         const int c0 = begin + (p.unit ? k : cost.before(k)), len = p.unit ? 1 : cost.a - cost.step * k;              // of the block
         pc.row0 = (cost.blocks - 1 - k) * kRows;
-        const bool narrow = !kWide || rows <= kNarrow;
+        const bool narrow = rows <= kNarrow;
         const int last_row = (pc.row0 + kRows < rows ? pc.row0 + kRows : rows) - 1;
         const Span span = span_of(rq.p0 + (pc.row0 >> p.gs), rq.p0 + (last_row >> p.gs), rq.limit, p.window, p.n_sink);
         pc.from = 0;
@@ -492,7 +491,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
         bool some = true;                                           // the piece has tiles, or is the only one
         if (!p.unit) {
             // cost offset -> tile: what lies behind the idle part, cut at every fourth (wide blocks are worked on four at a time)
-            const int idle = Cost<NW, kWide>::idle(rows), round = 4;
+            const int idle = Cost<NW>::idle(rows), round = 4;
             auto tile_at = [&](int off) { const int t = off - idle; return t <= 0 ? 0 : off >= len ? span.n : t / round * round < span.n ? t / round * round : span.n; };
             all.start = c0 >= share * size ? share : c0 / size;
             all.last = c0 + len <= (share + 1) * size ? share : (c0 + len - 1) / size;
@@ -517,13 +516,12 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
             };
             const int64_t slot = all.slot(p, share, g);
             if (narrow) {
-                const int some_rows = last_row + 1 - pc.row0;
                 narrow_sums<NW>(sums, p, pc, span, s_all + At::tiles, (int*)s_notes);
                 claim();
                 // the waves' sums meet: rows of 32 x 16 bytes per wave, turned by the row (banks)
                 const int n = lane & 31, kh = lane >> 5;
                 float4_t* s_sum = (float4_t*)(s_all + At::tiles);
-                if (n < some_rows) {
+                if (n < rows) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int c4 = 8 * (i >> 2) + 2 * (i & 3) + kh;
@@ -533,8 +531,8 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
                     if (kh == 0) s_stat[wave * kNarrow + n] = float4_t{sums.m_ref, sums.l, sums.s_max, 0.f};
                 }
                 __syncthreads();
-                for (int u = tid; u < some_rows * (kD / 2); u += kThreads) {             // two channels to a lane
-                    const int row = u >> 6, c2 = u & 63, of = pc.row0 + row, t = rq.t0 + (of >> p.gs), h = (g << p.gs) + (of & (p.G - 1));
+                for (int u = tid; u < rows * (kD / 2); u += kThreads) {             // two channels to a lane
+                    const int row = u >> 6, c2 = u & 63, t = rq.t0 + (row >> p.gs), h = (g << p.gs) + (row & (p.G - 1));
                     float m = kNegBig, s_max = kMasked, sum = 0.f;
                     float4_t st[NW];
 #pragma unroll
@@ -569,9 +567,8 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
                     }
                 }
                 if (pieces > 1 && last_to_arrive(word, p.tag, pieces, &s_flag))
-                    for (int row = wave; row < some_rows; row += NW)
-                        merge_row(p, all, row, g, rq.t0 + (pc.row0 + row >> p.gs), (g << p.gs) + (pc.row0 + row & (p.G - 1)), lane);
-            } else if constexpr (kWide) {
+                    for (int row = wave; row < rows; row += NW) merge_row(p, all, row, g, rq.t0 + (row >> p.gs), (g << p.gs) + (row & (p.G - 1)), lane);
+            } else {
                 wide_sums<NW, true>(sums, p, pc, span, s_all + At::tiles, &s_odd, s_notes);
                 claim();
                 const int row = pc.row0 + 32 * wave + (lane & 31);
@@ -623,7 +620,7 @@ size_t page_attn_workspace_bytes(const Geom& g, int64_t T)
     return most;
 }
 
-template <int NW, bool kWide>
+template <int NW>
 static hipError_t launch_t(const Geom& g, Params& p, int64_t T, void* ws, hipStream_t st)
 {
     p.shares = shares_of(g, NW);
@@ -633,10 +630,9 @@ static hipError_t launch_t(const Geom& g, Params& p, int64_t T, void* ws, hipStr
     p.done = (unsigned long long*)ws;
     p.part_out = (float*)((char*)ws + align_up((size_t)pairs * sizeof(unsigned long long)));
     p.part_stat = p.part_out + 2 * pairs * p.rows_cap * kD;
-    constexpr int kRows = Cost<NW, kWide>::kRows;
-    const int64_t most = T * g.G / kRows + (g.B < T ? g.B : T);             // blocks that there can be
+    const int64_t most = T * g.G / (32 * NW) + (g.B < T ? g.B : T);         // blocks that there can be
     p.unit = unit_blocks(g, T, most, p.table_cap << p.shift);
-    hipLaunchKernelGGL((page_attn_kernel<NW, kWide>), dim3((unsigned)((p.unit ? most : p.shares) * g.Hkv)), dim3(NW * 64), 0, st, p);
+    hipLaunchKernelGGL(page_attn_kernel<NW>, dim3((unsigned)((p.unit ? most : p.shares) * g.Hkv)), dim3(NW * 64), 0, st, p);
     return hipGetLastError();
 }
 
@@ -648,8 +644,7 @@ hipError_t launch_page_attn(const Geom& g, const Pages& pg, const PageAttnArgs& 
     p.c1 = a.scale * kLog2e; p.Hkv = g.Hkv; p.G = g.G; p.gs = log2_of(g.G); p.window = a.window; p.n_sink = a.n_sink;
     p.q_start = a.q_start; p.ctx_len = a.ctx_len; p.table = a.table; p.table_cap = a.table_cap; p.n_pages = pg.n;
     p.T = (int)a.T; p.R = g.B; p.shift = pg.shift;
-    if (a.T <= g.B) return launch_t<4, false>(g, p, a.T, ws, st);
-    return waves_of(g, a.T) == 8 ? launch_t<8, true>(g, p, a.T, ws, st) : launch_t<4, true>(g, p, a.T, ws, st);
+    return waves_of(g, a.T) == 8 ? launch_t<8>(g, p, a.T, ws, st) : launch_t<4>(g, p, a.T, ws, st);
 }
 
 }  // namespace antkv
