@@ -13,8 +13,8 @@
 // barrier; the waves' sums meet in LDS.
 //
 // Bound: many tokens, the matrix units (2048 on 32768 keys, 32 heads on 8, 1.02 ms, 1.04 PFLOP/s); one token each, HBM (64 requests on 1 .. 32768
-// keys 175 us, 4.6 TB/s); few keys or requests, the chain plan - pages - first tiles - meeting - partial sums - their sum, 1 to 3 us
-// each (one token on 4096 keys 15 us, of which its tiles take 5).
+// keys 147 us, 5.5 TB/s); few keys or requests, the chain plan - pages - first tiles - meeting - partial sums - their sum, 1 to 3 us
+// each (one token on 4096 keys 13 us, of which its tiles take 5).
 #include "span_attn.h"
 
 #include <type_traits>
@@ -70,9 +70,10 @@ struct Cost {
             if (p.window == 0 && q.p0 >= 0 && q.p0 + q.n <= q.limit) step = kRows / 32 >> p.gs;
         }
     }
-    // Key tiles' worth of coming and going: looking up pages, the first loads, partial sums.  64 requests of a token on 1 .. 32768 keys with
-    // 4, 20, 28: 208, 176, 178 us; 16 requests, some with hundreds of tokens, with 10, 12, 16, 20 for their wide blocks: 92, 87.5, 87.6, 89
-    __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? 20 : 16; }
+    // Key tiles' worth of coming and going: looking up pages, the first loads, partial sums.  Narrow 14, 20, 28: 16
+    // tokens on 300 keys each 11.0, 15.0, 16.2 us, 63 tokens beside one chunk of 100 on 2000 keys each 105, 106, 118, 64 on 1 .. 32768 keys 147, 148,
+    // 147 (4, measured earlier: 208 where 20 took 176).  Wide 12, 16, 20: 300 tokens on 2000 keys 46, 38, 46, 8 prompts of 1024 131, 121, 119
+    __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? 14 : 16; }
     __device__ __forceinline__ int before(int k) const { return k * a - step * (k * (k - 1) / 2); }      // of blocks 0 .. k - 1
     __device__ __forceinline__ int all() const { return before(blocks); }
     __device__ __forceinline__ int block_at(int x) const            // the block in which x lies
@@ -441,8 +442,8 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
     int size = 1, x = share, end = total;                           // the share: costs x .. end - 1 (unit: block x)
     if (!p.unit) {
         size = (total + p.shares - 1) / p.shares;
-        // Less is not worth the partial sums.  4, 12, 24: a token on 4096 keys 20.8, 16.3, 17.3 us; 16, 24, 48, 96: 64 tokens on 4096 keys 35,
-        // 36, 44, 68, 300 on 2000 44, 42, 59, 93, 4 x 100 on 1000 36, 34, 43, 56
+        // Less is not worth the partial sums.  8, 12, 16: a token on 4096 keys 14.7, 13.2, 13.8 us, one each of 4 requests on 2048 keys 16.6,
+        // 14.5, 14.9; 16, 24, 32: 64 tokens on 4096 keys 32.5, 33.9, 36.0, 300 on 2000 39.4, 38.1, 46.2, 4 x 100 on 1000 32.1, 31.4, 32.0
         const int least = wide ? 24 : 12;
         if (size < least) size = least;
         x = share < p.shares ? share * size : total;
@@ -590,9 +591,10 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
 
 }  // namespace
 
-// Few long chunks: 8 waves read a key tile for 256 rows; many requests: 4 waves, two workgroups to a CU, one works while the other comes
-// or goes.  8 and 4 waves: a chunk of 2048 on 32768 keys 1.00 and 1.11 ms, one of 300 on 2000 42 and 44 us, 8 prompts of 1024 131 and 139, 4 of 100 on 1000 38 and 35, 16 requests with 2048 tokens among them (500 for four of
-// them, one for the others) on up to 8192 keys 97 and 88 us, 64 requests of a token each on up to 32768 keys 182 and 176, one on 4096 17.6 and 16.2.
+// Long chunks: 8 waves read a key tile for 256 rows; fewer tokens: 4 waves, two workgroups to a CU, one works while the other comes or
+// goes.  With 8 and 4 waves, 32 heads on 8: a chunk of 2048 on 32768 keys 998 and 1125 us, 8192 on 32768 3510 and 3645, 8 prompts of 1024 120 and 127,
+// 64 of 256 154 and 147, one of 300 on 2000 keys 38 and 35; 4 of 100 on 1000 38 and 32, 64 tokens on 4096 keys 45 and 34, 16 requests with 2048 tokens
+// among them (500 for four of them, one for the others) on up to 8192 keys 93 and 83, one token on 4096 14.5 and 13.2.
 static int waves_of(const Geom& g, int64_t T) { return T * g.G >= (int64_t)g.B * 1024 ? 8 : 4; }
 // Shares per KV head: the chip's workgroups, or one each.
 static int shares_of(const Geom& g, int nw) { return g.Hkv < kWaves / nw ? kWaves / nw / g.Hkv : 1; }
@@ -600,9 +602,10 @@ static int shares_of(const Geom& g, int nw) { return g.Hkv < kWaves / nw ? kWave
 static int rows_cap_of(const Geom& g, int64_t T, int nw) { return T * g.G < 32 * nw ? ((int)(T * g.G) + 31) / 32 * 32 : 32 * nw; }
 
 // A workgroup per block, where prompts are long and blocks two to a workgroup at least, so that nothing has to be cut: blocks of a prompt
-// that run at the same time are then on about the same keys, which come out of the L2.  In shares and in blocks, 32 heads, 8 KV heads: 16384
-// tokens 2190 and 2157 us, 8192 on 32768 keys 3790 and 3648, 4 x 4096 647 and 627, 8 x 2048 394 and 385, but 8 x 1024 131 and 142, 1000 x 100
-// 886 and 1349, 512 x 1 on 1024 keys 402 and 481.  Also where the costs of all blocks might not fit an int.
+// that run at the same time are then on about the same keys, which come out of the L2.  In shares and in blocks, 32 heads on 8: 16384
+// tokens 2108 and 2067 us, 8192 on 32768 keys 3618 and 3510, 4 x 4096 616 and 595, 8 x 2048 369 and 350, 4 x 2048 on 2048 .. 16384 834 and 789, but
+// 8 x 1024 123 and 132, 1000 x 100 838 and 1201, 4096 tokens on 100 keys each 539 and 1540.  Also where the costs of all blocks might not
+// fit an int.
 static bool unit_blocks(const Geom& g, int64_t T, int64_t most, int64_t longest)
 {
     return (T >= 2048 * (int64_t)g.B && T * g.G / 256 * g.Hkv >= 2 * kWaves / 8) || most > (1LL << 30) / (longest / 32 + 32);
