@@ -10,7 +10,7 @@ using namespace span;
 
 // Matrix instructions bound it where windows are long, coming and going (the query rows, the first tiles, the last ones) where they are
 // short.  Waves of a workgroup: four, so that a CU holds two and one computes while the other comes or goes; 8 and 4 measured, us, 32 heads:
-// 8192 tokens, 8 KV heads, window 1024: 183 and 177 (130 GFLOP, 735 TFLOP/s); 16384, window 4096: 1026 and 993 (969 TFLOP/s); 2 x 1531, 32 KV heads,
+// 8192 tokens, 8 KV heads, window 1024: 183 and 177 (129 GFLOP, 730 TFLOP/s; 174 on another card); 16384, window 4096: 1026 and 993 (969 TFLOP/s); 2 x 1531, 32 KV heads,
 // window 256: 60 and 50; 4096, 32 KV heads, window 128: 67 and 56; 16384, window 16384: 2170 and 2123 (1036 TFLOP/s).
 constexpr int NW = 4;
 
