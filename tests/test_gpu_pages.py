@@ -303,7 +303,7 @@ def test_page_attn_wide_batch():
 
 
 def test_page_attn_a_workgroup_per_block():
-    """So many blocks that none of them is cut: many requests of few tokens, and a long prompt."""
+    """Many blocks: of many requests of few tokens, in shares, and of a long prompt, each a workgroup of its own."""
     rng = np.random.default_rng(4)
     ctx = rng.integers(1, 300, 300).tolist()
     check_attn(Cache(6, ctx, 8, 16), [1 + (r % 7 == 0) * min(c - 1, 40) for r, c in enumerate(ctx)], 16, each=3)
@@ -483,6 +483,33 @@ def test_page_attn_a_token_each_on_average(Hq, Hkv, window, n_sink):
     ctx = [600, 1, 70, 2000, 33, 64] + [5] * 94
     check_attn(Cache(61, ctx, Hkv, 32), [40, 1, 0, 33, 17, 0] + [0] * 90 + [5, 0, 1, 1], Hq, window, n_sink, pad=2)
     check_attn(Cache(62, [3000] + [9] * 129, Hkv, 16), [130] + [0] * 129, Hq, window, n_sink)
+
+
+def test_page_attn_as_many_requests_as_there_may_be():
+    """8192 requests, most of a token or none, in 128 looks at their lengths."""
+    rng = np.random.default_rng(71)
+    ctx = rng.integers(1, 60, 8192).tolist()
+    new = [0 if r % 5 == 0 else min(c, 1 + 30 * (r % 97 == 0)) for r, c in enumerate(ctx)]
+    ctx[8000], new[8000] = 5000, 70
+    c = Cache(71, ctx, 1, 16)
+    starts = np.concatenate([[0], np.cumsum(new)])
+    q, geom = randn(gen_of(71), int(starts[-1]), 2, D), antkv.Geometry(8192, 2, 1, 8)
+    out, top, total = antkv.page_attn(geom, q, SCALE, ints(starts), ints(ctx), c.table, c.k_pages, c.v_pages, want_stats=True)
+    assert out.isfinite().all()
+    for r in [*range(0, 8192, 97), 8000, 8191]:
+        a, b = int(starts[r]), int(starts[r + 1])
+        pos = torch.arange(ctx[r] - new[r], ctx[r], device="cuda")
+        for h in range(2 if new[r] else 0):
+            compare((out[a:b, h], top[h, a:b], total[h, a:b]), exact(q[a:b, h], c.k[r][0], c.v[r][0], pos, 0, 0), f"request {r}, head {h}")
+
+
+def test_page_attn_requests_that_share_pages():
+    """The same pages in the tables of three requests, as a common beginning."""
+    c = Cache(72, [100, 64, 80], 2, 16)
+    for r in (1, 2):
+        c.table[r, :4] = c.table[0, :4]
+        c.k[r][:, :64], c.v[r][:, :64] = c.k[0][:, :64], c.v[0][:, :64]
+    check_attn(c, [1, 20, 10], 8)
 
 
 def test_page_attn_tables_of_great_capacity():
