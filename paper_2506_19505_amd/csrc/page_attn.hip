@@ -327,9 +327,10 @@ __device__ __forceinline__ void merge_row(const Params& p, const Pieces& pc, int
             if (s1 > 0) fetch(s1);
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
-                const float ws = s1 + j < most ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (s1 + j) & 63)) : 0.f;
-                o0 = fmaf(v[j][0], ws, o0);
-                o1 = fmaf(v[j][1], ws, o1);
+                const float ws = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (s1 + j) & 63));
+                const bool there = s1 + j < most;                   // (what was read again for pieces that are none may be infinite)
+                o0 = fmaf(there ? v[j][0] : 0.f, there ? ws : 0.f, o0);
+                o1 = fmaf(there ? v[j][1] : 0.f, there ? ws : 0.f, o1);
             }
         }
     }

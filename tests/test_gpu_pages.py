@@ -691,3 +691,30 @@ def test_captured_step_replayed_with_other_lengths():
         assert torch.equal(pools[0], eager[3]) and torch.equal(pools[1], eager[4])
         assert torch.equal(out[:rows].view(torch.int16), eager[5][:rows].view(torch.int16)), f"replay {i}"
         assert out[:rows].isfinite().all()
+
+
+# ------------------------------------------------------------------------------------------------ visible infinities
+
+def one_way(gen, k, top, gain, rows, Hq):
+    """Queries all of about one direction, and keys k [Hkv, C, D] of which number `top` scores 16.3 gain log2 units more than the others."""
+    base = torch.where(torch.rand(D, device="cuda", generator=gen) < 0.5, 1.0, -1.0)
+    k.copy_((0.05 * k.float()).half())
+    if gain:
+        k[:, top] = (gain * base).half()
+    return (base + 0.1 * randn(gen, rows, Hq, D).float()).half()
+
+
+def spread_odd(v, keys):
+    """inf, -inf and NaN at the given keys of v [Hkv, C, D], each in a channel of its own, and one channel with inf and -inf."""
+    for i, key in enumerate(keys):
+        v[:, key, 7 * i + 1] = (float("inf"), -float("inf"), float("nan"))[i % 3]
+    v[:, keys[0], 127], v[:, keys[-1], 127] = float("inf"), -float("inf")
+
+
+@pytest.mark.parametrize("Hq,Hkv,ctx", [(8, 2, 5000), (1, 1, 1300), (4, 1, 20000)])
+def test_page_attn_infinities_in_pieces_of_a_row(Hq, Hkv, ctx):
+    """One token whose keys are cut into pieces, no multiple of 16 of them: an infinity in the last one, which is read again in place of those missing."""
+    c = Cache(81, [ctx], Hkv, 16)
+    spread_odd(c.v[0], [ctx - 40, ctx - 70, ctx - 100])
+    c.fill()
+    check_attn(c, [1], Hq)
