@@ -154,15 +154,17 @@ __device__ __forceinline__ void narrow_sums(Sums& sums, const Params& p, const P
     const Operands at(k_at, v_at, lane);
     half8_t tq[8];
     load_query(tq, p, x, row, lane);
+    const int32_t* row_of = p.table + (int64_t)x.r * p.table_cap;
+    auto place_at = [&](int tile, int j) {                          // of 16-key half j, -1: no page
+        int key = tile * 32 + 16 * j;
+        if (key > ((span.keys - 1) & ~15)) key = (span.keys - 1) & ~15;
+        return place_of(p, row_of, x.g, key);
+    };
+    bool odd = false;                                               // some edge tile's V was not finite
     for (int ua = x.from; ua < x.to; ua += kTurnNarrow) {
         const int m = x.to - ua < kTurnNarrow ? x.to - ua : kTurnNarrow;
-        const int32_t* row_of = p.table + (int64_t)x.r * p.table_cap;
         if (ua > x.from) __syncthreads();                           // the turn before has been read
-        for (int k = tid; k < 2 * m; k += NW * 64) {
-            int key = span.tile(ua + (k >> 1)) * 32 + 16 * (k & 1);
-            if (key > ((span.keys - 1) & ~15)) key = (span.keys - 1) & ~15;
-            s_place[k] = place_of(p, row_of, x.g, key);
-        }
+        for (int k = tid; k < 2 * m; k += NW * 64) s_place[k] = place_at(span.tile(ua + (k >> 1)), k & 1);
         wait_all_loads();
         __syncthreads();
         const int mine = (m - wave + NW - 1) / NW;                  // tiles wave, wave + NW, .. of the turn
@@ -179,7 +181,6 @@ __device__ __forceinline__ void narrow_sums(Sums& sums, const Params& p, const P
         vc = c = scalar(c);
         stage(p.k, a, c, tile_of(0) == last_tile, k_at);
         stage(p.v, a, c, tile_of(0) == last_tile, v_at);
-        bool odd = false;                                           // some edge tile's V was not finite
 #pragma unroll 1
         for (int i = 0; i < mine; ++i) {
             const int tile = tile_of(i);
@@ -214,7 +215,7 @@ __device__ __forceinline__ void narrow_sums(Sums& sums, const Params& p, const P
             }
             sums.l += sum[0] + sum[1];
             asm volatile("s_waitcnt vmcnt(8)" ::: "memory");         // V has landed
-            if (__builtin_expect(edge, 0)) {                        // hidden or not, what is not finite waits until the turn is over
+            if (__builtin_expect(edge, 0)) {                        // hidden or not, what is not finite waits until the end
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     lds_uint4* to = (lds_uint4*)(uintptr_t)(v_at + 1024 * j + lane * 16);
@@ -240,23 +241,25 @@ __device__ __forceinline__ void narrow_sums(Sums& sums, const Params& p, const P
             vc = c;
             stage(p.v, va, vc, more_last, v_at);
         }
-        if (__builtin_expect(odd, 0))
-            for (int i = 0; i < mine; ++i) {
-                places(i, a, c);
-                a = scalar(a);
-                c = scalar(c);
-                const uint32_t bits = (a < 0 ? 1 : 0) | (c < 0 ? 2 : 0);
-                if (bits == 0 && sight.whole(tile_of(i), all, hi)) continue;
-                wait_all_loads();
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                stage(p.v, a, c, tile_of(i) == last_tile, v_at);
-                wait_all_loads();
-                add_odd(sums, at, 0, sight.of_tile(tile_of(i), bits, kh));
-            }
         wait_all_loads();                                           // nothing may land in LDS after the turn
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     sums.join_halves();
+    // values that are not finite, to the rows that see them: of the wave's edge tiles, or of all where some sum is not finite
+    const bool every = __any(sums.odd());
+    if (__builtin_expect(odd || every, 0)) {
+        if (every) sums.drop_odd();
+#pragma unroll 1
+        for (int u = x.from + wave; u < x.to; u += NW) {
+            const int tile = span.tile(u), a = scalar(place_at(tile, 0)), c = scalar(place_at(tile, 1));
+            const uint32_t bits = (a < 0 ? 1 : 0) | (c < 0 ? 2 : 0);
+            if (!every && bits == 0 && sight.whole(tile, all, hi)) continue;
+            stage(p.v, a, c, tile == last_tile, v_at);
+            wait_all_loads();
+            add_odd(sums, at, 0, sight.of_tile(tile, bits, kh));
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the tile has been read
+        }
+    }
 }
 
 // ---- partial sums ----------------------------------------------------------------------------------------------------------------

@@ -20,6 +20,11 @@
 // value product of tile t - 1 (16 MFMAs), none of which waits for it.  Tiles that some row sees in part (the diagonal, the window's
 // left edge, the end of the sinks or of the context, a page that is none) are masked, and their V is looked at: what is not finite
 // must not reach the product of a row that does not see it (0 x inf).
+//
+// Values that are not finite.  A row that sees one has it in its result, whatever the weight; but a weight below 2^-25 is 0 in
+// fp16, one far enough below the largest 0 in fp32 too, and 0 x inf is NaN.  Tiles that all rows see are not looked at: their infinities leave
+// some sum that is not finite (none turns finite again), which is looked for once at the end.  Then, or where the tiles that were looked at held
+// some, V is gone through a second time, and the rows get inf, -inf or NaN by counting (add_odd): the result does not depend on where tiles begin.
 #pragma once
 
 #include "lds_tile.h"
@@ -151,6 +156,24 @@ struct Sums {
     {
         l += __shfl_xor(l, 32, 64);
         s_max = fmaxf(s_max, __shfl_xor(s_max, 32, 64));
+    }
+    // Some sum is not finite although the row's weights are numbers (halves joined): a value that the row sees is not.  Sums of finite
+    // values are at most 2^15 x 2^16 x 2^30.
+    __device__ __forceinline__ bool odd() const
+    {
+        float t = 0.f;
+#pragma unroll
+        for (int cg = 0; cg < 4; ++cg)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) t = fmaf(o[cg][r], 0.f, t);
+        return t != t && l == l;
+    }
+    __device__ __forceinline__ void drop_odd()
+    {
+#pragma unroll
+        for (int cg = 0; cg < 4; ++cg)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[cg][r] = l == l && !(fabsf(o[cg][r]) < INFINITY) ? 0.f : o[cg][r];
     }
 };
 
@@ -329,6 +352,14 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
     half8_t tq[8], pr[2][2];
     load_query(tq, p, x, row, lane);
     float16_t sc[2];
+    auto place_at = [&](int tile, int j) {                          // of 16-key half j, -1: no page
+        int key = tile * 32 + 16 * j;
+        if (key > ((span.keys - 1) & ~15)) key = (span.keys - 1) & ~15;
+        return kPaged ? place_of(p, p.table + (int64_t)x.r * p.table_cap, x.g, key) : key >> 4;
+    };
+    auto noted = [&](int place, int tile) { return (place < 0 ? kBad : place << 2) | (tile == last_tile ? kLast : 0); };
+    auto seen_by_all = [&](int tile) { return sight.whole(tile, sees_to(x.row0), stands_at(x.row0 + 32 * NW - 1)); };
+    if (tid == 0) *s_odd = 0;
 
     for (int ua = x.from; ua < x.to; ua += kTurn) {
         const int m = x.to - ua < kTurn ? x.to - ua : kTurn;        // tiles of this turn; i counts them
@@ -341,13 +372,11 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
             int bad = 0;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                int key = tile * 32 + 16 * j, place;
-                if (key > ((span.keys - 1) & ~15)) key = (span.keys - 1) & ~15;
-                place = kPaged ? place_of(p, p.table + (int64_t)x.r * p.table_cap, x.g, key) : key >> 4;
+                const int place = place_at(tile, j);
                 bad |= place < 0;
-                note.place[j] = (place < 0 ? kBad : place << 2) | (tile == last_tile ? kLast : 0);
+                note.place[j] = noted(place, tile);
             }
-            if (bad || !sight.whole(tile, sees_to(x.row0), stands_at(x.row0 + 32 * NW - 1))) {
+            if (bad || !seen_by_all(tile)) {
                 note.edge |= kEdgeAny;
                 for (int w = 0; w < NW; ++w)
                     if (bad || !sight.whole(tile, sees_to(x.row0 + 32 * w), stands_at(x.row0 + 32 * w + 31))) note.edge |= 1 << w;
@@ -355,7 +384,6 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
             note.unused = 0;
             notes[i] = note;
         }
-        if (tid == 0) *s_odd = 0;
         // the V slot of "tile -1" is multiplied with zero probabilities: it has to be finite
 #pragma unroll
         for (int i = 0; i < kParts; ++i) *(uint4_t*)(s_kv + (2 * kRing - 1) * kTileBytes + (i * NW * 64 + tid) * 16) = uint4_t{0u, 0u, 0u, 0u};
@@ -403,7 +431,7 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
             return scalar(note.edge) & kHidden ? 0u : sight.of_tile(tile_of(i), bad, kh);
         };
         // A hidden key counts as nothing whatever its V holds, but 0 x inf is NaN: in a tile of which some row of the workgroup does not
-        // see some key, V that is not finite is cleared in LDS, by the wave that has staged it, and looked at again after the turn.
+        // see some key, V that is not finite is cleared in LDS, by the wave that has staged it, and looked at again at the end.
         const uint32_t own = lds0 + (kRing * kTileBytes) + wave * (kParts * 1024) + lane * 16;       // what the lane has staged of a V tile
         auto clear_odd = [&](int slot) __attribute__((always_inline)) {
 #pragma unroll
@@ -490,21 +518,27 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
                 land(i & 3, edge);
             }
         }
-        // the cleared values of the turn, to the rows that see them
-        if (__builtin_expect(scalar(*s_odd), 0)) {
-            for (int i = 0; i < m; ++i) {
-                if (!(scalar(notes[i].edge) & kEdgeAny)) continue;
-                wait_all_loads();
-                __syncthreads();
-                stage(vbase, own_place(i), kRing);
-                wait_all_loads();
-                __syncthreads();
-                if (active) add_odd(sums, at, 0, seen_of(i));
-            }
-        }
         wait_all_loads();                                           // nothing may land in LDS after the turn, or the workgroup's end
     }
     sums.join_halves();
+    // values that are not finite, to the rows that see them: 1, some were cleared; 2, some sum is not finite
+    if (active && __any(sums.odd())) *s_odd = 2;
+    __syncthreads();
+    const int odd = scalar(*s_odd);
+    if (__builtin_expect(odd, 0)) {
+        if (odd == 2) sums.drop_odd();
+#pragma unroll 1
+        for (int u = x.from; u < x.to; ++u) {
+            const int tile = span.tile(u), p0 = scalar(place_at(tile, 0)), p1 = scalar(place_at(tile, 1));
+            const uint32_t bad = (p0 < 0 ? 1 : 0) | (p1 < 0 ? 2 : 0);
+            if (odd == 1 && bad == 0 && seen_by_all(tile)) continue;
+            stage(vbase, noted(half ? p1 : p0, tile), kRing);
+            wait_all_loads();
+            __syncthreads();
+            if (active) add_odd(sums, at, 0, sight.of_tile(tile, bad, kh));
+            __syncthreads();                                        // the tile has been read
+        }
+    }
 }
 
 // A row's result: fp16 channels 32 cg + 8 qd + 4 kh .. + 3 and, from half-wave 0, its statistics.  A row that sees nothing is zero.

@@ -718,3 +718,32 @@ def test_page_attn_infinities_in_pieces_of_a_row(Hq, Hkv, ctx):
     spread_odd(c.v[0], [ctx - 40, ctx - 70, ctx - 100])
     c.fill()
     check_attn(c, [1], Hq)
+
+
+@pytest.mark.parametrize("top", [5, 170])
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (150, 70)])
+@pytest.mark.parametrize("ctx,new", [([300], [1]), ([300], [300]), ([290, 300], [60, 1])])
+def test_page_attn_infinities_of_little_weight(ctx, new, window, n_sink, top):
+    """A value that a row sees is in its result whatever its weight: 65 log2 units below the largest (nothing, in fp16), in a tile that all
+    rows see and in one that some do."""
+    c = Cache(82, ctx, 2, 16)
+    q = torch.cat([one_way(gen_of(82 + r), c.k[r], top, 4, n, 8) for r, n in enumerate(new)])
+    for v in c.v:
+        spread_odd(v, [3, 40, 100, 150, 171, 220, 280])
+    c.fill()
+    check_attn(c, new, 8, window, n_sink, q=q)
+
+
+@pytest.mark.parametrize("gain", [4, 24])
+@pytest.mark.parametrize("N,Nq,window,n_sink,top", [(500, 500, 300, 40, 20), (500, 500, 500, 0, 400), (33000, 40, 32990, 33, 17000), (33000, 40, 32990, 33, 20)])
+def test_prefill_attn_window_infinities_of_little_weight(N, Nq, window, n_sink, top, gain):
+    """The same over a dense prompt, up to 391 log2 units (nothing, in fp32), and over more key tiles than are looked up at a time: the softmax
+    reference moves that far after, or long before, the value is seen."""
+    gen = gen_of(83)
+    k, v = randn(gen, 2, N, D), randn(gen, 2, N, D)
+    q = one_way(gen, k, top, gain, Nq, 4)
+    spread_odd(v, [2, 50, N // 2 - 10, N // 2 + 300 if N > 1000 else 260, N - 100, N - 64, N - 5])
+    q = q.transpose(0, 1).contiguous()
+    out, row_max, row_sum = antkv.prefill_attn_window(antkv.Geometry(1, 4, 2, 8), q[None], k[None], v[None], SCALE, window, n_sink)
+    for h in range(4):
+        compare((out[0, h], row_max[0, h], row_sum[0, h]), exact(q[h], k[h // 2], v[h // 2], torch.arange(N - Nq, N, device="cuda"), window, n_sink), f"head {h}")
