@@ -297,6 +297,10 @@ __device__ __forceinline__ bool last_to_arrive(unsigned long long* word, uint64_
     return scalar(*s_flag) != 0;
 }
 
+// Weight of sums at reference `from` beside others at `to` >= from.  Never 0, which would make NaN of an infinity that is among the sums: what
+// 2^-126 leaves of finite ones, at most 2^61, is nothing beside a weight of 2^8 or more, that of the largest score.
+__device__ __forceinline__ float weight(float from, float to) { return fmaxf(fast_exp2(from - to), 1.17549435e-38f); }
+
 // Adds the partial sums of a row of a narrow block: a wave, two channels to a lane.
 __device__ __forceinline__ void merge_row(const Params& p, const Pieces& pc, int row, int g, int64_t t, int h, int lane)
 {
@@ -318,12 +322,10 @@ __device__ __forceinline__ void merge_row(const Params& p, const Pieces& pc, int
             for (int j = 0; j < kBatch; ++j) v[j] = load_part(p.part_out + at(s0 + (s1 + j < most ? s1 + j : most - 1)) * kD + 2 * lane);
         };
         fetch(0);
-        const bool some = x[1] != 0.f;                              // (also where it is NaN)
         s_max = fmaxf(s_max, wave_max(y[0]));
-        const float m_new = fmaxf(m, wave_max(some ? x[0] : kNegBig)), back = fast_exp2(m - m_new);
-        const float w = some ? fast_exp2(x[0] - m_new) : 0.f;
+        const float m_new = fmaxf(m, wave_max(x[0])), back = weight(m, m_new), w = weight(x[0], m_new);
         m = m_new;
-        l = l * back + wave_sum(some ? x[1] * w : 0.f);
+        l = l * back + wave_sum(x[1] * w);
         o0 *= back;
         o1 *= back;
         for (int s1 = 0; s1 < most; s1 += kBatch) {
@@ -376,11 +378,10 @@ __device__ __forceinline__ void merge_wide(const Params& p, Sums& x, const Piece
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] = load_part(wide_part(p, slot, wave, i, lane));
         }
-        const bool some = u[1] != 0.f;                              // (also where it is NaN)
-        const float m_new = some ? fmaxf(all.m_ref, u[0]) : all.m_ref, back = fast_exp2(all.m_ref - m_new), w = some ? fast_exp2(u[0] - m_new) : 0.f;
+        const float m_new = fmaxf(all.m_ref, u[0]), back = weight(all.m_ref, m_new), w = weight(u[0], m_new);
         all.m_ref = m_new;
         all.s_max = fmaxf(all.s_max, v[0]);
-        all.l = all.l * back + (some ? u[1] * w : 0.f);
+        all.l = all.l * back + u[1] * w;
 #pragma unroll
         for (int i = 0; i < 32; ++i)
 #pragma unroll
@@ -543,14 +544,14 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
 #pragma unroll
                     for (int w = 0; w < NW; ++w) {
                         st[w] = s_stat[w * kNarrow + row];
-                        if (st[w][1] != 0.f) m = fmaxf(m, st[w][0]);
+                        m = fmaxf(m, st[w][0]);
                         s_max = fmaxf(s_max, st[w][2]);
                     }
                     float2_t o = {0.f, 0.f};
 #pragma unroll
                     for (int w = 0; w < NW; ++w) {
-                        const float f = st[w][1] != 0.f ? fast_exp2(st[w][0] - m) : 0.f;       // (a sum of NaN counts)
-                        if (f != 0.f) sum = fmaf(st[w][1], f, sum);
+                        const float f = weight(st[w][0], m);
+                        sum = fmaf(st[w][1], f, sum);
                         const float2_t v = ((const float2_t*)&s_sum[(w * kNarrow + row) * 32 + (((c2 >> 1) + row) & 31)])[c2 & 1];
                         o[0] = fmaf(v[0], f, o[0]);
                         o[1] = fmaf(v[1], f, o[1]);

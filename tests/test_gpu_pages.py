@@ -747,3 +747,30 @@ def test_prefill_attn_window_infinities_of_little_weight(N, Nq, window, n_sink, 
     out, row_max, row_sum = antkv.prefill_attn_window(antkv.Geometry(1, 4, 2, 8), q[None], k[None], v[None], SCALE, window, n_sink)
     for h in range(4):
         compare((out[0, h], row_max[0, h], row_sum[0, h]), exact(q[h], k[h // 2], v[h // 2], torch.arange(N - Nq, N, device="cuda"), window, n_sink), f"head {h}")
+
+
+@pytest.mark.parametrize("gain", [0, 4, 24])
+@pytest.mark.parametrize("ctx,new,top", [([300], [1], 5), ([300], [1], 170), ([6000], [1], 10), ([6000], [1], 4000), ([9000], [100], 30), ([9000], [100], 5000),
+                                         ([4000, 5000], [1, 200], 3000)])
+def test_page_attn_infinities_where_sums_meet(ctx, new, top, gain):
+    """Sums of waves and of pieces whose weights beside the others are nothing in fp32 (391 log2 units) hold infinities: they stay."""
+    c = Cache(84, ctx, 2, 16)
+    q = torch.cat([one_way(gen_of(84 + r), c.k[r], top, gain, n, 8) for r, n in enumerate(new)])
+    for r, v in enumerate(c.v):
+        n = ctx[r]
+        spread_odd(v, [3, 45, n // 3, n // 2, n - 250, n - 100, n - 6])
+    c.fill()
+    check_attn(c, new, 8, q=q)
+
+
+@pytest.mark.parametrize("gain", [0, 4, 24])
+def test_page_attn_infinities_in_turns_of_a_row(gain):
+    """A token on more key tiles than a workgroup looks up at a time, all of them its own (a table of great capacity)."""
+    c = Cache(85, [40000] + [20] * 39, 1, 256)
+    q = torch.cat([one_way(gen_of(85), c.k[0], 36000, gain, 1, 4), randn(gen_of(86), 39, 4, D)])
+    spread_odd(c.v[0], [3, 20000, 32700, 33000, 36001, 39990])
+    c.fill()
+    table = torch.full((40, 1 << 22), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.table.shape[1]] = c.table
+    c.table = table
+    check_attn(c, [1] * 40, 4, q=q)
