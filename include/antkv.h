@@ -32,7 +32,8 @@
  *     errors are detected on the host before anything is enqueued.
  *   - Tensors are dense, row-major, last index fastest, in the layouts given per call.
  *     fp16 = IEEE binary16.  "KV head g of query head h" is g = h / (Hq / Hkv).
- *   - Geometry: D must be 128 and Hq / Hkv in {1, 2, 4}; M = D / d_sub sub-spaces per head.  Two code formats:
+ *   - Geometry: D must be 128, Hq / Hkv in {1, 2, 4} and B * Hkv at most 65535 (2^20 in the calls on pages); any other is
+ *     EUNSUPPORTED everywhere.  M = D / d_sub sub-spaces per head.  Two code formats:
  *       n_centroids 256, d_sub in {4, 8, 16}: one byte per code (2 / 1 / 0.5 bit per element, the paper's
  *         d4m256 / d8m256 notation, Sec. 4); every entry point supports it.
  *       n_centroids 4096, d_sub 32 or 16: 12-bit codes (0.375 / 0.75 bit per element, the d32m4096 and d16m4096
@@ -296,7 +297,8 @@ int antkv_prefill_attn_window(const antkv_geom* geom, const void* q, const void*
  * int32 [R][table_cap]; its slot number is page * page_size + j % page_size, and n_pages * page_size must be below 2^31,
  * table_cap * page_size at most 2^30.  Lengths, tables and slots live on the device and are read when the kernels run: a captured
  * step can be replayed with other lengths as long as its sizes (R, T, table_cap) hold them.  Page numbers outside [0, n_pages) and slots outside
- * the pool are never followed.  These calls read B, Hq, Hkv and D of the geometry; d_sub and n_centroids are not used but must be valid.
+ * the pool are never followed.  These calls read B, Hq, Hkv and D of the geometry, B * Hkv at most 2^20; d_sub and n_centroids are not
+ * used but must be valid.
  */
 
 /*

@@ -555,7 +555,10 @@ def page_load(geom: Geometry, k_pages: torch.Tensor, v_pages: torch.Tensor, tabl
 def page_attn_workspace(geom: Geometry, T: int, device) -> torch.Tensor:
     """A workspace of antkv_page_attn_workspace(geom, T) bytes for page_attn, for calls that follow each other on one stream with up to
     T rows."""
-    return _workspace(load_library().antkv_page_attn_workspace(geom._c, T), device)
+    nbytes = load_library().antkv_page_attn_workspace(geom._c, T)
+    if nbytes == 0 and T != 0 and geom.B != 0:
+        raise ValueError(f"page_attn does not take {T} rows of this geometry")
+    return _workspace(nbytes, device)
 
 
 def page_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Tensor, ctx_len: torch.Tensor, table: torch.Tensor,
@@ -581,7 +584,7 @@ def page_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Tens
     if want_stats:
         row_max, row_sum = torch.empty((2, Hq, T), dtype=torch.float32, device=q.device).unbind(0)
     if workspace is None:
-        workspace = page_attn_workspace(geom, T, q.device)
+        workspace = _workspace(load_library().antkv_page_attn_workspace(geom._c, T), q.device)
     else:
         _need(workspace, torch.uint8, "workspace")
     _run(load_library().antkv_page_attn, "antkv_page_attn", _one_device(q, k_pages, v_pages, q_start, ctx_len, table, out, workspace), geom._c,

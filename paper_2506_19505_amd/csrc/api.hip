@@ -7,7 +7,10 @@ using namespace antkv;
 
 namespace {
 
-int check_geom(const antkv_geom* gm, Geom& g)
+constexpr int64_t kMostPairs = 65535;                   // B * Hkv: the second axis of a grid
+constexpr int64_t kMostPagedPairs = 1LL << 20;          // of the calls on pages: 8192 requests of 128 KV heads
+
+int check_geom(const antkv_geom* gm, Geom& g, int64_t most_pairs = kMostPairs)
 {
     if (!gm) return ANTKV_EINVAL;
     if (gm->B < 0 || gm->Hq <= 0 || gm->Hkv <= 0 || gm->D <= 0 || gm->d_sub <= 0 || gm->n_centroids <= 0)
@@ -19,7 +22,7 @@ int check_geom(const antkv_geom* gm, Geom& g)
     if (!wide && !byte_codes) return ANTKV_EUNSUPPORTED;
     const int G = gm->Hq / gm->Hkv;
     if (G != 1 && G != 2 && G != 4) return ANTKV_EUNSUPPORTED;
-    if ((int64_t)gm->B * gm->Hkv > 65535) return ANTKV_EUNSUPPORTED;
+    if ((int64_t)gm->B * gm->Hkv > most_pairs) return ANTKV_EUNSUPPORTED;
     g.B = gm->B; g.Hq = gm->Hq; g.Hkv = gm->Hkv; g.G = G; g.d = gm->d_sub; g.M = kD / gm->d_sub;
     g.C = gm->n_centroids;
     g.code_bytes = wide ? 3 * g.M / 2 : g.M;
@@ -329,7 +332,7 @@ int antkv_page_store(const antkv_geom* geom, const void* k, const void* v, int64
                      void* k_pages, void* v_pages, int64_t n_pages, int32_t page_size, void* stream)
 {
     Geom g;
-    int rc = check_geom(geom, g);
+    int rc = check_geom(geom, g, kMostPagedPairs);
     if (rc) return rc;
     Pages pg;
     rc = check_pages(n_pages, page_size, pg);
@@ -349,7 +352,7 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
                     int64_t xs_b, int64_t xs_h, int64_t xs_t, void* stream)
 {
     Geom g;
-    int rc = check_geom(geom, g);
+    int rc = check_geom(geom, g, kMostPagedPairs);
     if (rc) return rc;
     Pages pg;
     rc = check_pages(n_pages, page_size, pg);
@@ -367,7 +370,7 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
 size_t antkv_page_attn_workspace(const antkv_geom* geom, int64_t T)
 {
     Geom g;
-    if (check_geom(geom, g) || g.B > kMapRequests || T < 1 || T > (1LL << 30) / g.Hq || g.B == 0) return 0;
+    if (check_geom(geom, g, kMostPagedPairs) || g.B > kMapRequests || T < 1 || T > (1LL << 30) / g.Hq || g.B == 0) return 0;
     return page_attn_workspace_bytes(g, T);
 }
 
@@ -377,7 +380,7 @@ int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t
                     float* row_sum, void* workspace, size_t workspace_bytes, void* stream)
 {
     Geom g;
-    int rc = check_geom(geom, g);
+    int rc = check_geom(geom, g, kMostPagedPairs);
     if (rc) return rc;
     Pages pg;
     rc = check_pages(n_pages, page_size, pg);

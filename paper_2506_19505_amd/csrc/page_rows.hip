@@ -16,6 +16,7 @@ constexpr int kThreads = 256;
 constexpr int kLanes = kD * 2 / 16;                                 // lanes of a row
 constexpr int kRows = 2;                                            // rows of a thread
 constexpr int kSpan = kThreads / kLanes * kRows;                    // rows of a workgroup
+constexpr int kMostRows = 65535;                                    // of workgroups, the second axis of a grid
 
 // row of slot `slot`, head g, in 16-byte pieces
 __device__ __forceinline__ int64_t page_row(int64_t page, int off, int g, int Hkv, int shift)
@@ -55,39 +56,41 @@ __global__ __launch_bounds__(kThreads) void page_store_kernel(const uint4_t* __r
 
 __global__ __launch_bounds__(kThreads) void page_load_kernel(const uint4_t* __restrict__ k_pages, const uint4_t* __restrict__ v_pages, int64_t n_pages,
                                                              int shift, const int32_t* __restrict__ table, int64_t table_cap,
-                                                             const int32_t* __restrict__ ctx_len, int64_t first, int64_t N, int Hkv,
+                                                             const int32_t* __restrict__ ctx_len, int64_t first, int64_t N, int B, int Hkv,
                                                              uint4_t* __restrict__ k, uint4_t* __restrict__ v, int64_t xs_b, int64_t xs_h,
                                                              int64_t xs_t)
 {
     const int lane = threadIdx.x % kLanes;
-    const int b = blockIdx.y / Hkv, g = blockIdx.y % Hkv;
-    int64_t end = first + N;
-    if (ctx_len && ctx_len[b] < end) end = ctx_len[b];
-    const int64_t to = b * xs_b + g * xs_h + lane;
-    for (int64_t t0 = (int64_t)blockIdx.x * kSpan + threadIdx.x / kLanes; t0 < N; t0 += (int64_t)gridDim.x * kSpan) {
-        uint4_t x[kRows], y[kRows];
-        bool have[kRows];
+    for (int pair = blockIdx.y; pair < B * Hkv; pair += gridDim.y) {
+        const int b = pair / Hkv, g = pair % Hkv;
+        int64_t end = first + N;
+        if (ctx_len && ctx_len[b] < end) end = ctx_len[b];
+        const int64_t to = b * xs_b + g * xs_h + lane;
+        for (int64_t t0 = (int64_t)blockIdx.x * kSpan + threadIdx.x / kLanes; t0 < N; t0 += (int64_t)gridDim.x * kSpan) {
+            uint4_t x[kRows], y[kRows];
+            bool have[kRows];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int64_t pos = first + t0 + i * (kThreads / kLanes);
-            have[i] = false;
-            if (pos < end) {
-                const int64_t page = table[b * table_cap + (pos >> shift)];
-                if (page >= 0 && page < n_pages) {
-                    const int64_t from = page_row(page, (int)(pos & ((1 << shift) - 1)), g, Hkv, shift) + lane;
-                    x[i] = k_pages[from];
-                    y[i] = v_pages[from];
-                    have[i] = true;
+            for (int i = 0; i < kRows; ++i) {
+                const int64_t pos = first + t0 + i * (kThreads / kLanes);
+                have[i] = false;
+                if (pos < end) {
+                    const int64_t page = table[b * table_cap + (pos >> shift)];
+                    if (page >= 0 && page < n_pages) {
+                        const int64_t from = page_row(page, (int)(pos & ((1 << shift) - 1)), g, Hkv, shift) + lane;
+                        x[i] = k_pages[from];
+                        y[i] = v_pages[from];
+                        have[i] = true;
+                    }
                 }
             }
-        }
 #pragma unroll
-        for (int i = 0; i < kRows; ++i)
-            if (have[i]) {
-                const int64_t at = to + (t0 + i * (kThreads / kLanes)) * xs_t;
-                k[at] = x[i];
-                v[at] = y[i];
-            }
+            for (int i = 0; i < kRows; ++i)
+                if (have[i]) {
+                    const int64_t at = to + (t0 + i * (kThreads / kLanes)) * xs_t;
+                    k[at] = x[i];
+                    v[at] = y[i];
+                }
+        }
     }
 }
 
@@ -108,8 +111,9 @@ hipError_t launch_page_load(int B, int Hkv, const Pages& pg, const half_t* k_pag
 {
     int64_t blocks = (N + kSpan - 1) / kSpan;
     if (blocks > 1 << 20) blocks = 1 << 20;
-    hipLaunchKernelGGL(page_load_kernel, dim3((unsigned)blocks, (unsigned)(B * Hkv)), dim3(kThreads), 0, st, (const uint4_t*)k_pages,
-                       (const uint4_t*)v_pages, pg.n, pg.shift, table, table_cap, ctx_len, first, N, Hkv, (uint4_t*)k, (uint4_t*)v, xs_b / 8, xs_h / 8,
+    const int pairs = B * Hkv < kMostRows ? B * Hkv : kMostRows;
+    hipLaunchKernelGGL(page_load_kernel, dim3((unsigned)blocks, (unsigned)pairs), dim3(kThreads), 0, st, (const uint4_t*)k_pages,
+                       (const uint4_t*)v_pages, pg.n, pg.shift, table, table_cap, ctx_len, first, N, B, Hkv, (uint4_t*)k, (uint4_t*)v, xs_b / 8, xs_h / 8,
                        xs_t / 8);
     return hipGetLastError();
 }

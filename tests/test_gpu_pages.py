@@ -774,3 +774,26 @@ def test_page_attn_infinities_in_turns_of_a_row(gain):
     table[:, :c.table.shape[1]] = c.table
     c.table = table
     check_attn(c, [1] * 40, 4, q=q)
+
+
+# ------------------------------------------------------------------------------------------------ many requests of many heads
+
+def test_as_many_requests_as_there_may_be_of_eight_heads():
+    """8192 requests on 8 KV heads, more than 65535 pairs of them: attention, and their rows out of the pages."""
+    rng = np.random.default_rng(91)
+    R, Hkv, page = 8192, 8, 16
+    ctx = rng.integers(1, 40, R).tolist()
+    new = [0 if r % 5 == 0 else min(c, 1 + 30 * (r % 97 == 0)) for r, c in enumerate(ctx)]
+    c = Cache(91, ctx, Hkv, page, extra=0)
+    starts = np.concatenate([[0], np.cumsum(new)])
+    q, geom = randn(gen_of(91), int(starts[-1]), 2 * Hkv, D), antkv.Geometry(R, 2 * Hkv, Hkv, 8)
+    out, top, total = antkv.page_attn(geom, q, SCALE, ints(starts), ints(ctx), c.table, c.k_pages, c.v_pages, want_stats=True)
+    k, v = antkv.page_load(geom, c.k_pages, c.v_pages, c.table, 39, ctx_len=ints(ctx))
+    assert out.isfinite().all()
+    for r in [*range(0, R, 97), R - 2, R - 1]:
+        a, b = int(starts[r]), int(starts[r + 1])
+        pos = torch.arange(ctx[r] - new[r], ctx[r], device="cuda")
+        for h in range(r % 3, 2 * Hkv if new[r] else 0, 3):
+            compare((out[a:b, h], top[h, a:b], total[h, a:b]), exact(q[a:b, h], c.k[r][h // 2], c.v[r][h // 2], pos, 0, 0), f"request {r}, head {h}")
+        assert torch.equal(k[r, :, :ctx[r]], c.k[r]) and torch.equal(v[r, :, :ctx[r]], c.v[r])
+        assert (k[r, :, ctx[r]:] == 0).all() and (v[r, :, ctx[r]:] == 0).all()

@@ -128,3 +128,23 @@ def test_batches_beyond_a_grid(lib):
     assert lib.antkv_page_attn_workspace(ctypes.byref(_g()), (1 << 27) + 1) == 0 < lib.antkv_page_attn_workspace(ctypes.byref(_g()), 1 << 27)
     assert _attn(lib, g=one, n_pages=1 << 26) == EINVAL              # (2^33 rows of a head)
     assert _window(lib, N=1 << 30, Nq=1 << 30) == _window(lib, g=one, N=1 << 30, Nq=1 << 30) == _window(lib, g=one, N=1 << 28, Nq=1 << 28) == EINVAL
+
+
+def test_as_many_pairs_of_request_and_head_as_there_may_be(lib):
+    """8192 requests of ordinary numbers of heads: what is refused here is the workspace, or nothing is to be done."""
+    for B, hkv in ((8192, 8), (2048, 32), (8192, 128)):
+        g = _g(B=B, Hq=hkv, Hkv=hkv)
+        assert lib.antkv_page_attn_workspace(ctypes.byref(g), 8192) > 0
+        assert _attn(lib, g=g, wsb=1000) == EWORKSPACE
+        assert _load(lib, g=g, N=0) == _store(lib, g=g, T=0) == _attn(lib, g=g, T=0) == OK
+    g = _g(B=8192, Hq=129, Hkv=129)
+    assert lib.antkv_page_attn_workspace(ctypes.byref(g), 1) == 0
+    assert _load(lib, g=g, N=0) == _store(lib, g=g, T=0) == _attn(lib, g=g, T=0) == EUNSUPPORTED
+    assert _window(lib, g=_g(B=8192, Hq=8, Hkv=8), q=None) == EUNSUPPORTED
+
+
+def test_a_workspace_that_would_be_refused_is_not_made():
+    for geom, T in ((antkv.Geometry(8193, 8, 2, 8), 1), (antkv.Geometry(1, 8, 2, 8), 1 << 28), (antkv.Geometry(1, 6, 1, 8), 4), (antkv.Geometry(1, 8, 2, 8), -1)):
+        with pytest.raises(ValueError):
+            antkv.page_attn_workspace(geom, T, "cpu")
+    assert antkv.page_attn_workspace(antkv.Geometry(1, 8, 2, 8), 0, "cpu").numel() > 0
