@@ -325,7 +325,7 @@ int antkv_page_map(int64_t R, const int32_t* held_len, const int32_t* new_len, i
 /*
  * Row t of k and v (fp16 [T][Hkv][D], both with element strides xs_t, xs_h, channel stride 1; 16-byte aligned, strides multiples of
  * 8) goes to slot[t] of the pools.  Rows whose slot is negative or behind the pool are skipped.  Slots of one call are distinct:
- * a slot that is given twice holds pieces of either row.  T * Hkv is at most 2^29.  T == 0 is a no-op.  Errors: EINVAL, EUNSUPPORTED, ELAUNCH.
+ * a slot that is given twice holds pieces of either row.  T * Hkv is at most 2^29 - 32.  T == 0 is a no-op.  Errors: EINVAL, EUNSUPPORTED, ELAUNCH.
  */
 int antkv_page_store(const antkv_geom* geom, const void* k, const void* v, int64_t xs_t, int64_t xs_h, int64_t T,
                      const int32_t* slot, void* k_pages, void* v_pages, int64_t n_pages, int32_t page_size, void* stream);

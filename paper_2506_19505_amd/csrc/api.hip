@@ -337,7 +337,7 @@ int antkv_page_store(const antkv_geom* geom, const void* k, const void* v, int64
     Pages pg;
     rc = check_pages(n_pages, page_size, pg);
     if (rc) return rc;
-    if (T < 0 || T > (1LL << 29) / g.Hkv) return ANTKV_EINVAL;
+    if (T < 0 || T > kMostBlocks * 32 / g.Hkv) return ANTKV_EINVAL;      // (a workgroup has 32 rows)
     if (T == 0) return ANTKV_OK;
     if (!k || !v || !slot || !k_pages || !v_pages || k_pages == v_pages) return ANTKV_EINVAL;
     if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16)) return ANTKV_EINVAL;

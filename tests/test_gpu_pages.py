@@ -797,3 +797,19 @@ def test_as_many_requests_as_there_may_be_of_eight_heads():
             compare((out[a:b, h], top[h, a:b], total[h, a:b]), exact(q[a:b, h], c.k[r][h // 2], c.v[r][h // 2], pos, 0, 0), f"request {r}, head {h}")
         assert torch.equal(k[r, :, :ctx[r]], c.k[r]) and torch.equal(v[r, :, :ctx[r]], c.v[r])
         assert (k[r, :, ctx[r]:] == 0).all() and (v[r, :, ctx[r]:] == 0).all()
+
+
+def test_page_store_of_the_largest_batch():
+    """As many rows as a grid has, all of them the same one and nearly all without a slot."""
+    T, Hkv = (1 << 23) - 1, 64
+    gen = gen_of(92)
+    k, v = (randn(gen, 1, Hkv, D).expand(T, Hkv, D) for _ in "kv")
+    kp, vp = (torch.zeros((4, Hkv, 16, D), dtype=torch.float16, device="cuda") for _ in "kv")
+    slot = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    slot[0], slot[T // 2], slot[-1] = 5, 63, 30
+    antkv.page_store(antkv.Geometry(1, Hkv, Hkv, 8), k, v, slot, kp, vp)
+    for x, pages in ((k, kp), (v, vp)):
+        want = torch.zeros_like(pages)
+        for s in (5, 63, 30):
+            want[s // 16, :, s % 16] = x[0]
+        assert torch.equal(pages, want)

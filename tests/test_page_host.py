@@ -148,3 +148,9 @@ def test_a_workspace_that_would_be_refused_is_not_made():
         with pytest.raises(ValueError):
             antkv.page_attn_workspace(geom, T, "cpu")
     assert antkv.page_attn_workspace(antkv.Geometry(1, 8, 2, 8), 0, "cpu").numel() > 0
+
+
+@pytest.mark.parametrize("hkv", [1, 2, 64])
+def test_page_store_of_a_grid_and_a_row_more(lib, hkv):
+    """2^29 rows are 2^24 workgroups of 256 threads, 2^32 threads: one workgroup too many."""
+    assert _store(lib, g=_g(Hq=hkv, Hkv=hkv), T=(1 << 29) // hkv) == EINVAL
