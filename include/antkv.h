@@ -285,7 +285,9 @@ int antkv_prefill_attn(const antkv_geom* geom, const void* q, const void* k, con
  * its own among them) or j < n_sink (the first tokens of the context, which stay visible).  window >= 1, n_sink >= 0; either may
  * exceed N.  K or V that a query does not see has no influence on its row, whatever it holds, infinities and NaN among it; a value
  * (V) that it sees and that is not finite is in its row as inf, -inf or NaN, however small the weight.
- * N up to 2^30.  Otherwise as antkv_prefill_attn.
+ * N up to 2^30.  row_max and row_sum are of the keys that the row sees: antkv_anchor_select, which knows no window, must not be given
+ * them where the window hides a key (weights of hidden keys would not be probabilities; it makes its own without them).
+ * Otherwise as antkv_prefill_attn.  Errors: EINVAL, EUNSUPPORTED, ELAUNCH.
  */
 int antkv_prefill_attn_window(const antkv_geom* geom, const void* q, const void* k, const void* v, int64_t N, int64_t Nq,
                               float scale, int64_t window, int64_t n_sink, void* out, float* row_max, float* row_sum,
@@ -349,8 +351,8 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
  *   q        fp16 [T][Hq][D] with element strides qs_t, qs_h (multiples of 8), 16-byte aligned
  *   q_start  int32 [R + 1] ascending from 0 (otherwise rows between its entries may stay as they are);  ctx_len int32 [R];  table as above
  *   out      fp16 [T][Hq][D]; accumulation is fp32, rounded once; probabilities enter the value product rounded to fp16
- *   row_max, row_sum  optional fp32 [Hq][T] (both or neither) as antkv_prefill_attn's: for a single request the layout that
- *            antkv_anchor_select takes with Nq = T
+ *   row_max, row_sum  optional fp32 [Hq][T] (both or neither) as antkv_prefill_attn's, of the keys that the row sees: for a single request the
+ *            layout that antkv_anchor_select takes with Nq = T.  It knows no window: statistics of a window that hides a key must not go there
  * Rows of T behind q_start[R] are left as they are.  Keys on pages that are none, and positions behind the table's end, are not
  * seen; a row that sees nothing is zero, with row_max -inf and row_sum 0.  What a row does not see has no influence on it, whatever it
  * holds (pages need not be cleared); a value (V) that it sees and that is not finite is in it as inf, -inf or NaN, however small

@@ -461,7 +461,8 @@ def _table(t: torch.Tensor, requests: int) -> int:
 def prefill_attn_window(geom: Geometry, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, window: int, n_sink: int = 0,
                         want_stats: bool = True):
     """antkv_prefill_attn_window: prefill_attn in which a query sees the last `window` positions and the first `n_sink`.
-    q fp16 [B,Hq,Nq,D], k / v fp16 [B,Hkv,N,D] -> (out fp16 [B,Hq,Nq,D], row_max, row_sum)."""
+    q fp16 [B,Hq,Nq,D], k / v fp16 [B,Hkv,N,D] -> (out fp16 [B,Hq,Nq,D], row_max, row_sum).  The statistics are of the keys that a row
+    sees: not for anchor_select where the window hides some."""
     _need(q, torch.float16, "q")
     _need(k, torch.float16, "k")
     _need(v, torch.float16, "v")
@@ -566,7 +567,8 @@ def page_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Tens
               want_stats: bool = False, workspace: torch.Tensor | None = None):
     """antkv_page_attn: q fp16 [T,Hq,D] (channels contiguous), q_start int32 [R+1], ctx_len int32 [R], table int32 [R,cap], pools
     fp16 [n_pages,Hkv,page_size,D], geom.B = R -> (out fp16 [T,Hq,D], row_max, row_sum fp32 [Hq,T] or None).
-    Rows of out behind q_start[R] are left as they are (undefined where out is made here)."""
+    Rows of out behind q_start[R] are left as they are (undefined where out is made here).  The statistics are of the keys that a row sees:
+    not for anchor_select where a window hides some."""
     Hq, R = geom.Hq, geom.B
     _rows(q, "q", Hq)
     n_pages, page_size = _pools(k_pages, v_pages, geom.Hkv)
