@@ -813,3 +813,64 @@ def test_page_store_of_the_largest_batch():
         for s in (5, 63, 30):
             want[s // 16, :, s % 16] = x[0]
         assert torch.equal(pages, want)
+
+
+# ------------------------------------------------------------------------------------------------ replays over other pieces
+
+@pytest.mark.parametrize("most", [1, 100])
+def test_captured_step_replayed_over_other_numbers_of_pieces(most):
+    """A step captured in two graphs that share a workspace, replayed over contexts whose lengths change places and size: a share's arrival
+    word meets blocks of 9, 3, 8 and one piece (tokens of their own: contexts of 3000 and 900 end in share 15, or 12, by turns), of single
+    tokens, and with a chunk of 100 among them."""
+    Hq, Hkv, page, R, own = 8, 2, 16, 4, 200
+    T = R - 1 + most
+    gen, geom = gen_of(93), antkv.Geometry(R, Hq, Hkv, 8)
+    n_pages = R * own + 40
+    pools = [randn(gen, n_pages, Hkv, page, D) for _ in "kv"]
+    order = torch.randperm(n_pages, device="cuda", generator=gen).to(torch.int32)
+    whole, free = order[:R * own].view(R, own), order[R * own:].contiguous()
+    table, held, new = whole.clone(), ints([0] * R), ints([1] * R)
+    q, k, v = randn(gen, T, Hq, D), randn(gen, T, Hkv, D), randn(gen, T, Hkv, D)
+    ws = antkv.page_attn_workspace(geom, T, "cuda")
+    out = torch.empty((T, Hq, D), dtype=torch.float16, device="cuda")
+
+    def step(table, kp, vp, out, ws):
+        lens, q_start, slot, _ = antkv.page_map(held, new, table, page, n_pages, free, T)
+        antkv.page_store(geom, k, v, slot, kp, vp)
+        antkv.page_attn(geom, q, SCALE, q_start, lens, table, kp, vp, out=out, workspace=ws)
+
+    step(table, *pools, out, ws)                                    # (loads the library)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(table, *pools, out, ws)
+        graphs.append(graph)
+    lengths = [[3000, 900, 40, 5], [5, 40, 900, 3000], [40, 3000, 5, 900], [900, 5, 3000, 40], [20, 30, 5, 40], [700, 5, 40, 2900], [2900, 40, 5, 700],
+               [3000, 5, 40, 900], [1, 15, 60, 3000]]
+    for i in range(2 * len(lengths)):                               # (an odd number of them: each goes to both graphs)
+        ctx = lengths[i % len(lengths)]
+        fresh = [1] * R
+        fresh[int(np.argmax(ctx)) if i % 3 else int(np.argsort(ctx)[-2])] = most
+        held.copy_(ints([max(c - n, 0) for c, n in zip(ctx, fresh)]))
+        new.copy_(ints(fresh))
+        table.copy_(whole)
+        for x in (q, k, v):
+            x.normal_()
+        eager = [t.clone() for t in (table, *pools, out)]
+        step(*eager, antkv.page_attn_workspace(geom, T, "cuda"))
+        graphs[i & 1].replay()
+        torch.cuda.synchronize()
+        for got, want in zip((table, *pools, out), eager):
+            assert torch.equal(got.view(torch.int16), want.view(torch.int16)), f"replay {i}"
+        assert out.isfinite().all()
+    cache = [p.clone() for p in pools]                              # the last step against 64 bits
+    ctx, starts = [max(c, n) for c, n in zip(ctx, fresh)], np.concatenate([[0], np.cumsum(fresh)])
+    for r in range(R):
+        j = torch.arange(ctx[r], device="cuda")
+        kr, vr = (p[table[r].long()[j // page], :, j % page].transpose(0, 1) for p in cache)
+        a, b = int(starts[r]), int(starts[r + 1])
+        for h in range(Hq):
+            want = exact(q[a:b, h], kr[h // 4], vr[h // 4], j[ctx[r] - fresh[r]:], 0, 0)[0]
+            assert ((out[a:b, h].double() - want).norm(dim=-1) <= OUT_TOL * want.norm(dim=-1)).all(), (r, h)
