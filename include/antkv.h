@@ -284,7 +284,8 @@ int antkv_prefill_attn(const antkv_geom* geom, const void* q, const void* k, con
  * The same with a sliding window: the query at position p sees keys j <= p with j > p - window (the last `window` positions,
  * its own among them) or j < n_sink (the first tokens of the context, which stay visible).  window >= 1, n_sink >= 0; either may
  * exceed N.  K or V that a query does not see has no influence on its row, whatever it holds, infinities and NaN among it; a value
- * (V) that it sees and that is not finite is in its row as inf, -inf or NaN, however small the weight.
+ * (V) that it sees and that is not finite is in its row as inf, -inf or NaN, however small the weight.  Scores (scale * q.k) of up to
+ * 2^26 in size; beyond that, where softmax references in fp32 come in steps of 16 powers of two, a row may come out as NaN or zero.
  * N up to 2^30.  row_max and row_sum are of the keys that the row sees: antkv_anchor_select, which knows no window, must not be given
  * them where the window hides a key (weights of hidden keys would not be probabilities; it makes its own without them).
  * Otherwise as antkv_prefill_attn.  Errors: EINVAL, EUNSUPPORTED, ELAUNCH.
@@ -356,7 +357,7 @@ int antkv_page_load(const antkv_geom* geom, const void* k_pages, const void* v_p
  * Rows of T behind q_start[R] are left as they are.  Keys on pages that are none, and positions behind the table's end, are not
  * seen; a row that sees nothing is zero, with row_max -inf and row_sum 0.  What a row does not see has no influence on it, whatever it
  * holds (pages need not be cleared); a value (V) that it sees and that is not finite is in it as inf, -inf or NaN, however small
- * the weight.  Sums have a fixed order: equal inputs give equal bits.
+ * the weight.  Scores of the size that antkv_prefill_attn_window allows.  Sums have a fixed order: equal inputs give equal bits.
  * T * Hq is at most 2^30, n_pages * Hkv * page_size below 2^32.  The workspace size is a function of Hq, Hkv, R and T; calls that share a workspace must not
  * overlap.  Errors: EINVAL, EUNSUPPORTED, EWORKSPACE, ELAUNCH.
  */

@@ -14,7 +14,8 @@
 //            through ds_read_b64_tr_b16.
 // Probabilities are exp2 against a per-row reference kLift below the largest score when it was set: it moves when a score comes
 // more than kPMax above it.  Rounded to fp16 they then keep 11 bits down to 2^-22 of the largest one and 2^-32 as a step, so that
-// many small weights beside a large one are not lost; their sum is taken before the rounding, in fp32.
+// many small weights beside a large one are not lost; their sum is taken before the rounding, in fp32.  The reference itself is rounded to fp32:
+// at scores of 2^27 log2 units to multiples of 16, which may lie 8 too low, and fp16 ends at 2^16.
 //
 // One step of the loop works on three tiles at once: the softmax of tile t (VALU) is interleaved with the scores of tile t + 1 and the
 // value product of tile t - 1 (16 MFMAs), none of which waits for it.  Tiles that some row sees in part (the diagonal, the window's

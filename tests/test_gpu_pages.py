@@ -874,3 +874,23 @@ def test_captured_step_replayed_over_other_numbers_of_pieces(most):
         for h in range(Hq):
             want = exact(q[a:b, h], kr[h // 4], vr[h // 4], j[ctx[r] - fresh[r]:], 0, 0)[0]
             assert ((out[a:b, h].double() - want).norm(dim=-1) <= OUT_TOL * want.norm(dim=-1)).all(), (r, h)
+
+
+# ------------------------------------------------------------------------------------------------ large scores
+
+@pytest.mark.parametrize("ctx,new", [([900], [1]), ([900], [300])])
+def test_scores_of_great_size(ctx, new):
+    """Scores of 4.5e7, at which log2 units come in steps of four: equal ones share the row, one above the others has it."""
+    gen, n = gen_of(94), new[0]
+    base = torch.where(torch.rand(D, device="cuda", generator=gen) < 0.5, 1.0, -1.0)
+    for tops in (range(900), [500], [3, 899], [40]):
+        c = Cache(94, ctx, 2, 16)
+        c.k[0].mul_(0.01)
+        c.k[0][:, list(tops)] = (2000 * base).half()
+        c.fill()
+        q = (2000 * base).half().expand(n, 8, D)
+        check_attn(c, new, 8, q=q)
+        dense = antkv.prefill_attn_window(antkv.Geometry(1, 8, 2, 8), q.transpose(0, 1)[None].contiguous(), c.k[0][None].contiguous(), c.v[0][None].contiguous(), SCALE, 700, 30)
+        pos = torch.arange(900 - n, 900, device="cuda")
+        for h in range(8):
+            compare([x[0, h] for x in dense], exact(q[:, h], c.k[0][h // 4], c.v[0][h // 4], pos, 700, 30), f"{tops} {h}")
