@@ -600,6 +600,9 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
 // goes.  With 8 and 4 waves, 32 heads on 8: a chunk of 2048 on 32768 keys 998 and 1125 us, 8192 on 32768 3510 and 3645, 8 prompts of 1024 120 and 127,
 // 64 of 256 154 and 147, one of 300 on 2000 keys 38 and 35; 4 of 100 on 1000 38 and 32, 64 tokens on 4096 keys 45 and 34, 16 requests with 2048 tokens
 // among them (500 for four of them, one for the others) on up to 8192 keys 93 and 83, one token on 4096 14.5 and 13.2.
+// The lengths are on the device, so that the host goes by the mean.  One long chunk among many short requests is on the slower side then, 2048 tokens on
+// 32768 keys beside 63 single tokens on 2000 each 1129 and 1185, beside 63 requests without a token 1018 and 1104; the same 63 beside 2048 tokens on
+// 4096 keys 220 and 192, beside 512 on 8192 183 and 149, 31 on 500 .. 16000 beside 2048 on 2048 275 and 219.
 static int waves_of(const Geom& g, int64_t T) { return T * g.G >= (int64_t)g.B * 1024 ? 8 : 4; }
 // Shares per KV head: the chip's workgroups, or one each.
 static int shares_of(const Geom& g, int nw) { return g.Hkv < kWaves / nw ? kWaves / nw / g.Hkv : 1; }
