@@ -65,6 +65,18 @@ __device__ __forceinline__ uint32_t wave_sum_u32(uint32_t v)
     for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
     return v;
 }
+// inclusive sum over the wave (register moves between lanes: within rows of 16, then across them)
+template <int kCtrl, int kMask>
+__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, kCtrl, kMask, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += from_lane<0x111, 0xf>(x);
+    x += from_lane<0x112, 0xf>(x);
+    x += from_lane<0x114, 0xf>(x);
+    x += from_lane<0x118, 0xf>(x);
+    x += from_lane<0x142, 0xa>(x);
+    return x + from_lane<0x143, 0xc>(x);
+}
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Wait until every global load issued so far has landed.  Placed after the loads of a loop-invariant register

@@ -92,18 +92,6 @@ struct Cost {
     }
 };
 
-// inclusive sums over the wave (register moves between lanes: within rows of 16, then across them)
-template <int kCtrl, int kMask>
-__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, kCtrl, kMask, 0xf, false); }
-__device__ __forceinline__ int wave_scan(int x)
-{
-    x += from_lane<0x111, 0xf>(x);
-    x += from_lane<0x112, 0xf>(x);
-    x += from_lane<0x114, 0xf>(x);
-    x += from_lane<0x118, 0xf>(x);
-    x += from_lane<0x142, 0xa>(x);
-    return x + from_lane<0x143, 0xc>(x);
-}
 __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
 // Where a workgroup is in the laid-out blocks: 64 requests at a time, one to a lane.  All other members are the same in every lane.

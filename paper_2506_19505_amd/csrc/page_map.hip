@@ -34,19 +34,7 @@ __device__ __forceinline__ int last_at_most(const int* s, int n, int x)
     return lo;
 }
 
-// inclusive sum over the wave (register moves between lanes: within rows of 16, then across them)
-template <int kCtrl, int kMask>
-__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, kCtrl, kMask, 0xf, false); }
-__device__ __forceinline__ int wave_scan(int x)
-{
-    x += from_lane<0x111, 0xf>(x);
-    x += from_lane<0x112, 0xf>(x);
-    x += from_lane<0x114, 0xf>(x);
-    x += from_lane<0x118, 0xf>(x);
-    x += from_lane<0x142, 0xa>(x);
-    return x + from_lane<0x143, 0xc>(x);
-}
-// of 31-bit numbers, in halves that cannot overflow
+// inclusive sum over the wave of 31-bit numbers, in halves that cannot overflow
 __device__ __forceinline__ int64_t wave_scan31(int x) { return ((int64_t)wave_scan(x >> 16) << 16) + wave_scan(x & 0xffff); }
 
 template <int kPer>                                     // slots of a thread: 4 where a request has many, which then are of one or two pages
