@@ -12,7 +12,7 @@
 // of its own through 16 KB of LDS, K of the next tile under the softmax of this one and V under the scores of the next, without a
 // barrier; the waves' sums meet in LDS.
 //
-// Bound: many tokens, the matrix units (2048 on 32768 keys, 32 heads on 8, 1.00 ms, 1.07 PFLOP/s); one token each, HBM (64 requests on 1 .. 32768
+// Bound: many tokens, the matrix units (2048 on 32768 keys, 32 heads on 8, 1.00 to 1.03 ms by card, 1.03 to 1.07 PFLOP/s); one token each, HBM (64 requests on 1 .. 32768
 // keys 147 us, 5.5 TB/s); few keys or requests, the chain plan - pages - first tiles - meeting - partial sums - their sum, 1 to 3 us
 // each (one token on 4096 keys 13 us, of which its tiles take 5).
 #include "span_attn.h"

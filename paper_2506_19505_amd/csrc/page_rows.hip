@@ -5,7 +5,7 @@
 //
 // Both are copies: 16 bytes per lane, 16 lanes to a row, K and V by the same thread.  A thread has its loads of kRows rows in
 // flight before it stores.  Bound: HBM, store 32768 tokens of 8 heads 55 us (4.85 TB/s read and written), load 4 x 32712 204 us
-// (5.26 TB/s); few rows: a launch and two dependent loads (64 tokens 2.8 us, 4099 6.6 us).
+// (5.26 TB/s); few rows: a launch and two dependent loads (64 tokens 2.8 us, 4099 6.4 us).
 #include "common.h"
 
 namespace antkv {
