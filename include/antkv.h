@@ -33,7 +33,7 @@
  *   - Tensors are dense, row-major, last index fastest, in the layouts given per call.
  *     fp16 = IEEE binary16.  "KV head g of query head h" is g = h / (Hq / Hkv).
  *   - Geometry: D must be 128, Hq / Hkv in {1, 2, 4} and B * Hkv at most 65535 (2^20 in the calls on pages); any other is
- *     EUNSUPPORTED everywhere.  M = D / d_sub sub-spaces per head.  Two code formats:
+ * *     refused everywhere.  M = D / d_sub sub-spaces per head.  Two code formats:
  *       n_centroids 256, d_sub in {4, 8, 16}: one byte per code (2 / 1 / 0.5 bit per element, the paper's
  *         d4m256 / d8m256 notation, Sec. 4); every entry point supports it.
  *       n_centroids 4096, d_sub 32 or 16: 12-bit codes (0.375 / 0.75 bit per element, the d32m4096 and d16m4096
