@@ -19,6 +19,8 @@
  *   antkv_page_store     new K / V rows to their slots
  *   antkv_page_attn      attention of each request's new tokens (one to thousands) over its pages, with row statistics
  *   antkv_page_load      a sequence's rows out of the pages, dense, as antkv_anchor_select and antkv_encode read them
+ *   antkv_qpage_store, antkv_qpage_load, antkv_qpage_attn   the same over pages of 8 bits, half the memory
+ *   antkv_rope           rotary positions of new Q and K rows, and back (antkv_rope_freqs: the frequencies)
  *   antkv_prefill_attn_window   prompt attention in which a query sees a window of recent keys and a few first ones
  *
  * Conventions
@@ -366,6 +368,72 @@ int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t
                     const int32_t* ctx_len, const int32_t* table, int64_t table_cap, const void* k_pages, const void* v_pages,
                     int64_t n_pages, int32_t page_size, float scale, int64_t window, int64_t n_sink, void* out, float* row_max,
                     float* row_sum, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same cache in 8 bits: half the memory and half the bytes of a step.  K and V are two pools uint8 [n_pages][Hkv][page_size][D] of e4m3
+ * values (a sign, four bits of exponent, three of mantissa; largest 448) and two arrays of scales fp32 [n_pages][Hkv][page_size / 16]: 16 slots of
+ * a KV head, a block, share one.  What a slot holds is its bytes' values x the scale of its block, an fp16 number always.  Tables, slots, lengths,
+ * limits and antkv_page_map are as above.
+ *
+ * antkv_qpage_store puts rows (k and v as in antkv_page_store) to their slots and makes the scales: powers of two, the least s = 2^-32 .. 2^8 with amax <= 448 s, amax the largest
+ * finite size among the block's rows.  A row's value x is then held as the nearest multiple, ties to even: off by at most |x| / 16, or 2^-10 s
+ * where |x| < 2^-6 s.  Sizes beyond 61440 count as 61440; infinities and NaN are held as NaN and have no part in the scale.
+ *   A block whose first slot is among the rows of the call begins anew: what it held is gone.  Otherwise it goes on: its scale grows if the new
+ *   rows need it, and rows that are there are rounded to the larger one (above 2^-6 of it that changes nothing; below it another 2^-10 s at
+ *   most, 2^-9 s over all times).  So positions of a request have to come in order, as antkv_page_map hands out their slots; a request that is cut back may
+ *   go on from any position.
+ *   The rows of a block lie within 16 rows of the batch that follow each other, in any order (positions in order do, also with some left out); slots of one call are
+ *   distinct.  A block whose rows lie further apart, or a slot given twice, leaves that block with undefined values.  The grid sets the limit of T: ceil(T / 16) * ceil(Hkv / 2) below 2^24.
+ * antkv_qpage_load is antkv_page_load: fp16 rows out.
+ * antkv_qpage_attn is antkv_page_attn over the values that antkv_qpage_load would give, to the same precision; its workspace size comes from
+ * antkv_qpage_attn_workspace.
+ * Scales that antkv_qpage_store has not made: antkv_qpage_load and antkv_qpage_attn take a positive normal number for the power of two at or below it; a block that goes
+ * on under one that is not among 2^-32 .. 2^8 goes on as under 2^-32.
+ */
+int antkv_qpage_store(const antkv_geom* geom, const void* k, const void* v, int64_t xs_t, int64_t xs_h, int64_t T, const int32_t* slot, void* k_pages,
+                      void* v_pages, float* k_scales, float* v_scales, int64_t n_pages, int32_t page_size, void* stream);
+int antkv_qpage_load(const antkv_geom* geom, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales, int64_t n_pages,
+                     int32_t page_size, const int32_t* table, int64_t table_cap, const int32_t* ctx_len, int64_t first, int64_t N, void* k, void* v,
+                     int64_t xs_b, int64_t xs_h, int64_t xs_t, void* stream);
+size_t antkv_qpage_attn_workspace(const antkv_geom* geom, int64_t T);
+int antkv_qpage_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t qs_h, int64_t T, const int32_t* q_start, const int32_t* ctx_len,
+                     const int32_t* table, int64_t table_cap, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                     int64_t n_pages, int32_t page_size, float scale, int64_t window, int64_t n_sink, void* out, float* row_max, float* row_sum,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions (Sec. 2.1 RoPE on Q and K; Sec. 3.3 last paragraph: keys before RoPE).  Of each row, pair i = 0 .. rot_dim / 2 - 1 of channels is
+ * turned by the angle position * freqs[i]:
+ *   y_a = amplitude * (x_a cos - x_b sin),   y_b = amplitude * (x_b cos + x_a sin)
+ * with (a, b) = (2 i, 2 i + 1) for rope_style 0, (i, i + rot_dim / 2) for rope_style 1 (as antkv_decode_attn_prerope's with rot_dim = D); channels from rot_dim on are
+ * copied.  inverse != 0 turns by the negative angle: with amplitude 1 / a it undoes a call with amplitude a (keys that were stored rotated, on
+ * their way into a codebook of keys before RoPE), with the same amplitude it is the gradient of that call.
+ *
+ *   q, k     fp16, either may be NULL (with its output): element (n, t, h, c) at n * xs_b + t * xs_t + h * xs_h + c; 16-byte aligned, strides
+ *            multiples of 8.  q has Hq heads, k Hkv.  Strides of an axis of length 1 are not looked at.
+ *   q_out, k_out  the same with strides of their own, each at least D; may be q and k themselves with equal strides.  Otherwise outputs must not overlap inputs
+ *            or each other.
+ *   positions, one of
+ *     pos               int32 [B][T]: of each row (any sign)
+ *     q_start, ctx_len  int32 [B + 1], [B] of a packed batch of T rows, as antkv_page_map makes them: row q_start[r] + i stands at
+ *                       ctx_len[r] - n + i, n its request's number of rows.  Batch strides are not used.  Rows outside the requests are left as they are.
+ *                       B at most 8192.
+ *     neither           pos0 + t, 0 <= pos0 <= 2^40
+ *   freqs    fp64 [rot_dim / 2], radians per position; rot_dim a multiple of 16 up to 128.  Angles are formed and reduced in fp64,
+ *            sine and cosine in fp32, y in fp32 and rounded once.
+ * B * T below 2^31; T == 0 is a no-op.  B, Hq, Hkv, D of the geometry are used, B * Hkv at most 2^20; d_sub must be valid.
+ *
+ * antkv_rope_freqs writes freqs (device memory): f_i = base^(-2 i / rot_dim), for contexts longer than the trained ones slowed down.
+ *   trained_len 0: all by `factor`, f_i / factor (factor 1: f_i).
+ *   trained_len > 0: by parts.  A pair that turns fast_turns times or more within trained_len positions keeps f_i, one that turns slow_turns times or less
+ *   gets f_i / factor, between them f_i (w + (1 - w) / factor) with w = (turns - slow_turns) / (fast_turns - slow_turns).
+ * Errors: EINVAL, EUNSUPPORTED (an even rot_dim that is no multiple of 16), ELAUNCH.
+ */
+int antkv_rope_freqs(int32_t rot_dim, double base, double factor, double trained_len, double slow_turns, double fast_turns, double* freqs, void* stream);
+int antkv_rope(const antkv_geom* geom, const void* q, int64_t qs_b, int64_t qs_t, int64_t qs_h, const void* k, int64_t ks_b, int64_t ks_t, int64_t ks_h,
+               int64_t T, const int32_t* pos, const int32_t* q_start, const int32_t* ctx_len, int64_t pos0, const double* freqs, int32_t rot_dim,
+               int32_t rope_style, float amplitude, int32_t inverse, void* q_out, int64_t qo_b, int64_t qo_t, int64_t qo_h, void* k_out, int64_t ko_b,
+               int64_t ko_t, int64_t ko_h, void* stream);
 
 /*
  * One iteration of the offline token-weighted k-means that learns a codebook (Sec. 3.1, "Offline Token-Aware

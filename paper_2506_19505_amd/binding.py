@@ -17,6 +17,7 @@ EXPORTS = (
     "antkv_topk_workspace", "antkv_topk", "antkv_gather_rows", "antkv_decode_attn_workspace", "antkv_decode_attn",
     "antkv_decode_attn_static", "antkv_set_decode_options", "antkv_decode_attn_prerope_workspace", "antkv_decode_attn_prerope", "antkv_append_token", "antkv_prefill_attn", "antkv_kmeans_step_workspace", "antkv_kmeans_step",
     "antkv_prefill_attn_window", "antkv_page_map", "antkv_page_store", "antkv_page_load", "antkv_page_attn_workspace", "antkv_page_attn",
+    "antkv_qpage_store", "antkv_qpage_load", "antkv_qpage_attn_workspace", "antkv_qpage_attn", "antkv_rope_freqs", "antkv_rope",
 )
 
 
@@ -121,6 +122,19 @@ def load_library():
         lib.antkv_page_attn_workspace.argtypes = [gp, i64]
         lib.antkv_page_attn.restype = ctypes.c_int
         lib.antkv_page_attn.argtypes = [gp, vp, i64, i64, i64, vp, vp, vp, i64, vp, vp, i64, i32, f32, i64, i64, vp, vp, vp, vp, sz, vp]
+        lib.antkv_qpage_store.restype = ctypes.c_int
+        lib.antkv_qpage_store.argtypes = [gp, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp, i64, i32, vp]
+        lib.antkv_qpage_load.restype = ctypes.c_int
+        lib.antkv_qpage_load.argtypes = [gp, vp, vp, vp, vp, i64, i32, vp, i64, vp, i64, i64, vp, vp, i64, i64, i64, vp]
+        lib.antkv_qpage_attn_workspace.restype = sz
+        lib.antkv_qpage_attn_workspace.argtypes = [gp, i64]
+        lib.antkv_qpage_attn.restype = ctypes.c_int
+        lib.antkv_qpage_attn.argtypes = [gp, vp, i64, i64, i64, vp, vp, vp, i64, vp, vp, vp, vp, i64, i32, f32, i64, i64, vp, vp, vp, vp, sz, vp]
+        f64 = ctypes.c_double
+        lib.antkv_rope_freqs.restype = ctypes.c_int
+        lib.antkv_rope_freqs.argtypes = [i32, f64, f64, f64, f64, f64, vp, vp]
+        lib.antkv_rope.restype = ctypes.c_int
+        lib.antkv_rope.argtypes = [gp, vp, i64, i64, i64, vp, i64, i64, i64, i64, vp, vp, vp, i64, vp, i32, i32, f32, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp]
         _lib = lib
     return _lib
 
@@ -594,3 +608,179 @@ def page_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Tens
          k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_size, float(scale), int(window), int(n_sink), out.data_ptr(), _p(row_max), _p(row_sum),
          workspace.data_ptr(), workspace.numel(), _stream(q))
     return out, row_max, row_sum
+
+
+# ---- the same cache in 8 bits -------------------------------------------------------------------------------------------
+
+def _byte_pools(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, heads: int):
+    _need(k_pages, torch.float8_e4m3fn, "k_pages")
+    _need(v_pages, torch.float8_e4m3fn, "v_pages")
+    _need(k_scales, torch.float32, "k_scales")
+    _need(v_scales, torch.float32, "v_scales")
+    shape = k_pages.shape
+    if len(shape) != 4 or shape[1] != heads or shape[3] != 128 or v_pages.shape != shape:
+        raise ValueError(f"k_pages and v_pages must be [n_pages, {heads}, page_size, 128]")
+    n_pages, page_size = shape[0], shape[2]
+    if k_scales.shape != (n_pages, heads, page_size // 16) or v_scales.shape != k_scales.shape:
+        raise ValueError(f"k_scales and v_scales must be [{n_pages}, {heads}, {page_size // 16}]")
+    return n_pages, page_size
+
+
+def qpage_store(geom: Geometry, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor,
+                v_scales: torch.Tensor) -> None:
+    """antkv_qpage_store: rows of k, v fp16 [T,Hkv,D] (equal strides, channels contiguous) to slot int32 [T] of pools
+    float8_e4m3fn [n_pages,Hkv,page_size,D] with scales fp32 [n_pages,Hkv,page_size/16]."""
+    heads = geom.Hkv
+    _rows(k, "k", heads)
+    n_pages, page_size = _byte_pools(k_pages, v_pages, k_scales, v_scales, heads)
+    T = k.shape[0]
+    if v.shape != k.shape or v.stride() != k.stride() or v.dtype is not torch.float16:
+        _rows(v, "v", heads)
+        if v.shape[0] != T or (T > 1 and v.stride(0) != k.stride(0)) or (heads > 1 and v.stride(1) != k.stride(1)):
+            raise ValueError("k and v must have the same shape and strides")
+    _ints(slot, "slot", (T,))
+    _run(load_library().antkv_qpage_store, "antkv_qpage_store", _one_device(k_pages, v_pages, k_scales, v_scales, k, v, slot), geom._c, k.data_ptr(),
+         v.data_ptr(), k.stride(0) if T > 1 else 0, k.stride(1) if heads > 1 else 0, T, slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+         k_scales.data_ptr(), v_scales.data_ptr(), n_pages, page_size, _stream(k_pages))
+
+
+def qpage_load(geom: Geometry, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, table: torch.Tensor, N: int,
+               first: int = 0, ctx_len: torch.Tensor | None = None, k: torch.Tensor | None = None, v: torch.Tensor | None = None):
+    """antkv_qpage_load: positions first .. first + N - 1 of the table's requests -> (k, v) fp16 [B,Hkv,N,D].  Rows at or behind
+    ctx_len (int32 [B]) are left as they are: zeros where k and v are made here."""
+    n_pages, page_size = _byte_pools(k_pages, v_pages, k_scales, v_scales, geom.Hkv)
+    cap = _table(table, geom.B)
+    if ctx_len is not None:
+        _ints(ctx_len, "ctx_len", (geom.B,))
+    shape = (geom.B, geom.Hkv, N, geom.D)
+    if k is None:
+        k = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
+    if v is None:
+        v = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
+    _need(k, torch.float16, "k")
+    _need(v, torch.float16, "v")
+    if k.shape != shape or v.shape != shape:
+        raise ValueError(f"k and v must be {list(shape)}")
+    rows = N * geom.D
+    _run(load_library().antkv_qpage_load, "antkv_qpage_load", _one_device(k_pages, v_pages, k_scales, v_scales, table, ctx_len, k, v), geom._c,
+         k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n_pages, page_size, table.data_ptr(), cap, _p(ctx_len), first, N,
+         k.data_ptr(), v.data_ptr(), geom.Hkv * rows, rows, geom.D, _stream(k_pages))
+    return k, v
+
+
+def qpage_attn_workspace(geom: Geometry, T: int, device) -> torch.Tensor:
+    """A workspace of antkv_qpage_attn_workspace(geom, T) bytes for qpage_attn, for calls that follow each other on one stream with up to
+    T rows."""
+    nbytes = load_library().antkv_qpage_attn_workspace(geom._c, T)
+    if nbytes == 0 and T != 0 and geom.B != 0:
+        raise ValueError(f"qpage_attn does not take {T} rows of this geometry")
+    return _workspace(nbytes, device)
+
+
+def qpage_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Tensor, ctx_len: torch.Tensor, table: torch.Tensor, k_pages: torch.Tensor,
+               v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, window: int = 0, n_sink: int = 0, out: torch.Tensor | None = None,
+               want_stats: bool = False, workspace: torch.Tensor | None = None):
+    """antkv_qpage_attn: page_attn over pools float8_e4m3fn [n_pages,Hkv,page_size,D] with scales fp32 [n_pages,Hkv,page_size/16]."""
+    Hq, R = geom.Hq, geom.B
+    _rows(q, "q", Hq)
+    n_pages, page_size = _byte_pools(k_pages, v_pages, k_scales, v_scales, geom.Hkv)
+    T = q.shape[0]
+    _ints(q_start, "q_start", (R + 1,))
+    _ints(ctx_len, "ctx_len", (R,))
+    cap = _table(table, R)
+    if out is None:
+        out = q.new_empty((T, Hq, 128))
+    else:
+        _need(out, torch.float16, "out")
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    row_max = row_sum = None
+    if want_stats:
+        row_max, row_sum = torch.empty((2, Hq, T), dtype=torch.float32, device=q.device).unbind(0)
+    if workspace is None:
+        workspace = _workspace(load_library().antkv_qpage_attn_workspace(geom._c, T), q.device)
+    else:
+        _need(workspace, torch.uint8, "workspace")
+    _run(load_library().antkv_qpage_attn, "antkv_qpage_attn", _one_device(q, k_pages, v_pages, k_scales, v_scales, q_start, ctx_len, table, out, workspace),
+         geom._c, q.data_ptr(), q.stride(0) if T > 1 else 0, q.stride(1) if Hq > 1 else 0, T, q_start.data_ptr(), ctx_len.data_ptr(), table.data_ptr(), cap,
+         k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n_pages, page_size, float(scale), int(window), int(n_sink),
+         out.data_ptr(), _p(row_max), _p(row_sum), workspace.data_ptr(), workspace.numel(), _stream(q))
+    return out, row_max, row_sum
+
+
+# ---- rotary positions ---------------------------------------------------------------------------------------------------
+
+def rope_freqs(rot_dim: int = 128, base: float = 10000.0, factor: float = 1.0, trained_len: float = 0, slow_turns: float = 1.0, fast_turns: float = 4.0,
+               device="cuda") -> torch.Tensor:
+    """antkv_rope_freqs: radians per position fp64 [rot_dim/2] for rope; base^(-2i/rot_dim), all of them / factor, or with a trained_len
+    only those that turn less than fast_turns times within it (wholly from slow_turns down)."""
+    freqs = torch.empty(max(int(rot_dim), 0) // 2, dtype=torch.float64, device=device)
+    if not freqs.is_cuda:
+        raise ValueError("freqs are made on a GPU")
+    _run(load_library().antkv_rope_freqs, "antkv_rope_freqs", freqs.get_device(), int(rot_dim), float(base), float(factor), float(trained_len),
+         float(slow_turns), float(fast_turns), freqs.data_ptr(), _stream(freqs))
+    return freqs
+
+
+def _rope_rows(x: torch.Tensor, out: torch.Tensor | None, name: str, heads: int, batch: int, packed: bool):
+    """x fp16 [T,heads,D] (packed, or one sequence) or [B,heads,T,D], channels contiguous -> (T, out, strides b, t, h of both)."""
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if x.dtype is not torch.float16:
+        raise TypeError(f"{name} must be torch.float16")
+    shape, d = x.shape, x.dim()
+    if d == 3 and (packed or batch == 1):
+        T, fits = shape[0], shape[1:] == (heads, 128)
+    elif d == 4 and not packed:
+        T, fits = shape[2], (shape[0], shape[1], shape[3]) == (batch, heads, 128)
+    else:
+        fits = False
+    if not fits or x.stride(-1) != 1:
+        raise ValueError(f"{name} must be " + (f"[T, {heads}, 128]" if packed else f"[{batch}, {heads}, T, 128]" + (f" or [T, {heads}, 128]" if batch == 1 else "")) +
+                         " with contiguous channels")
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float16, device=x.device)
+    elif out is not x:
+        if out.get_device() != x.get_device() or out.dtype is not torch.float16 or out.shape != shape or out.stride(-1) != 1:
+            raise ValueError(f"{name}_out must be like {name}")
+    a, b = x.stride(), out.stride()
+    return T, out, (0, a[0], a[1]) if d == 3 else (a[0], a[2], a[1]), (0, b[0], b[1]) if d == 3 else (b[0], b[2], b[1])
+
+
+def rope(geom: Geometry, q: torch.Tensor | None, k: torch.Tensor | None, freqs: torch.Tensor, pos: torch.Tensor | None = None,
+         q_start: torch.Tensor | None = None, ctx_len: torch.Tensor | None = None, pos0: int = 0, style: int = 0, amplitude: float = 1.0,
+         inverse: bool = False, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
+    """antkv_rope: q fp16 [T,Hq,D] and k [T,Hkv,D] of a packed batch (with q_start int32 [B+1] and ctx_len int32 [B], as page_map makes them) or of one
+    sequence, or [B,Hq,T,D] and [B,Hkv,T,D]; positions pos (int32, [T] or [B,T]) or pos0, pos0 + 1, ..; freqs fp64 [rot_dim/2] (rope_freqs) ->
+    (q_out, k_out), made here where they are not given; q_out=q turns q in place.  Rows outside a packed batch's requests are left as they
+    are (undefined where the output is made here)."""
+    packed = q_start is not None
+    _need(freqs, torch.float64, "freqs")
+    if freqs.dim() != 1:
+        raise ValueError("freqs must be [rot_dim / 2]")
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("q or k must be given")
+    T, none = None, (None, (0, 0, 0), (0, 0, 0))
+    rows = []
+    for x, out, name, heads in ((q, q_out, "q", geom.Hq), (k, k_out, "k", geom.Hkv)):
+        if x is None:
+            rows.append(none)
+            continue
+        n, *row = _rope_rows(x, out, name, heads, geom.B, packed)
+        if T is not None and (n != T or x.dim() != first.dim()):
+            raise ValueError("q and k must have the same rows")
+        T = n
+        rows.append(row)
+    if packed:
+        _ints(q_start, "q_start", (geom.B + 1,))
+        if ctx_len is None:
+            raise ValueError("q_start needs ctx_len")
+        _ints(ctx_len, "ctx_len", (geom.B,))
+    if pos is not None:
+        _ints(pos, "pos", (T,) if first.dim() == 3 else (geom.B, T))
+    (q_out, qs, qo), (k_out, ks, ko) = rows
+    _run(load_library().antkv_rope, "antkv_rope", _one_device(first, q, k, q_out, k_out, freqs, pos, q_start, ctx_len), geom._c, _p(q), *qs, _p(k), *ks, T,
+         _p(pos), _p(q_start), _p(ctx_len), int(pos0), freqs.data_ptr(), 2 * freqs.shape[0], int(style), float(amplitude), int(bool(inverse)), _p(q_out), *qo,
+         _p(k_out), *ko, _stream(first))
+    return q_out, k_out

@@ -45,6 +45,17 @@ constexpr int64_t kMostBlocks = (1LL << 24) - 1;        // of 256 threads: a gri
 // a block table of so many entries a row; positions stay below 2^30
 inline bool bad_table(int64_t table_cap, const Pages& pg) { return table_cap < 1 || table_cap > (1LL << 30) >> pg.shift; }
 
+// channels that turn: whole units of eight pairs
+inline bool bad_rot(int32_t rot) { return rot < 16 || rot > kD || (rot & 15) != 0; }
+// q or k of a call on rotary positions: 16-byte pieces; rows of the output do not overlap, in place means the same rows
+bool bad_rope_rows(const RopeRows& z, int64_t B, int64_t T, int heads)
+{
+    const int64_t x[3] = {z.xs_b, z.xs_t, z.xs_h}, y[3] = {z.ys_b, z.ys_t, z.ys_h}, n[3] = {B, T, heads};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && ((x[i] & 7) || x[i] < 0 || (y[i] & 7) || y[i] < kD || (z.x == z.y && x[i] != y[i]))) return true;
+    return misaligned(z.x, 16) || misaligned(z.y, 16);
+}
+
 struct SelPlan {
     size_t off_score, off_topk, total;
 };
@@ -374,10 +385,18 @@ size_t antkv_page_attn_workspace(const antkv_geom* geom, int64_t T)
     return page_attn_workspace_bytes(g, T);
 }
 
-int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t qs_h, int64_t T, const int32_t* q_start,
-                    const int32_t* ctx_len, const int32_t* table, int64_t table_cap, const void* k_pages, const void* v_pages,
-                    int64_t n_pages, int32_t page_size, float scale, int64_t window, int64_t n_sink, void* out, float* row_max,
-                    float* row_sum, void* workspace, size_t workspace_bytes, void* stream)
+size_t antkv_qpage_attn_workspace(const antkv_geom* geom, int64_t T)
+{
+    Geom g;
+    if (check_geom(geom, g, kMostPagedPairs) || g.B > kMapRequests || T < 1 || T > (1LL << 30) / g.Hq || g.B == 0) return 0;
+    return qpage_attn_workspace_bytes(g, T);
+}
+
+// scales: of pages of 8 bits, or none
+static int page_attn_impl(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t qs_h, int64_t T, const int32_t* q_start,
+                          const int32_t* ctx_len, const int32_t* table, int64_t table_cap, const void* k_pages, const void* v_pages,
+                          bool bytes, const float* k_scales, const float* v_scales, int64_t n_pages, int32_t page_size, float scale, int64_t window,
+                          int64_t n_sink, void* out, float* row_max, float* row_sum, void* workspace, size_t workspace_bytes, void* stream)
 {
     Geom g;
     int rc = check_geom(geom, g, kMostPagedPairs);
@@ -390,16 +409,117 @@ int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t
     if (n_pages * g.Hkv > 0x0fffffffLL / (page_size / 16)) return ANTKV_EINVAL;      // places of 16 rows: below 2^28, 1 TB
     if ((row_max == nullptr) != (row_sum == nullptr) || !(scale > 0.f)) return ANTKV_EINVAL;
     if (T == 0 || g.B == 0) return ANTKV_OK;
-    if (!q || !q_start || !ctx_len || !table || !k_pages || !v_pages || !out) return ANTKV_EINVAL;
+    if (!q || !q_start || !ctx_len || !table || !k_pages || !v_pages || !out || (bytes && (!k_scales || !v_scales))) return ANTKV_EINVAL;
     if (misaligned(q, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16) || misaligned(out, 16)) return ANTKV_EINVAL;
+    if (bytes && (misaligned(k_scales, 4) || misaligned(v_scales, 4))) return ANTKV_EINVAL;
     if ((qs_t & 7) || (qs_h & 7) || qs_t < 0 || qs_h < 0) return ANTKV_EINVAL;
-    if (!workspace || misaligned(workspace, 256) || workspace_bytes < page_attn_workspace_bytes(g, T)) return ANTKV_EWORKSPACE;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < (bytes ? qpage_attn_workspace_bytes(g, T) : page_attn_workspace_bytes(g, T))) return ANTKV_EWORKSPACE;
     PageAttnArgs a;
     a.q = (const half_t*)q; a.qs_t = qs_t; a.qs_h = qs_h; a.T = T; a.q_start = q_start; a.ctx_len = ctx_len; a.table = table;
     a.table_cap = table_cap; a.k_pages = (const half_t*)k_pages; a.v_pages = (const half_t*)v_pages; a.scale = scale;
     a.window = (int)window; a.n_sink = (int)(n_sink < 1LL << 30 ? n_sink : 1LL << 30);
     a.out = (half_t*)out; a.row_max = row_max; a.row_sum = row_sum;
-    return launch_page_attn(g, pg, a, workspace, (hipStream_t)stream) == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+    a.k_scales = k_scales; a.v_scales = v_scales;
+    const hipError_t e = bytes ? launch_qpage_attn(g, pg, a, workspace, (hipStream_t)stream) : launch_page_attn(g, pg, a, workspace, (hipStream_t)stream);
+    return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+}
+
+int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t qs_h, int64_t T, const int32_t* q_start,
+                    const int32_t* ctx_len, const int32_t* table, int64_t table_cap, const void* k_pages, const void* v_pages,
+                    int64_t n_pages, int32_t page_size, float scale, int64_t window, int64_t n_sink, void* out, float* row_max,
+                    float* row_sum, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return page_attn_impl(geom, q, qs_t, qs_h, T, q_start, ctx_len, table, table_cap, k_pages, v_pages, false, nullptr, nullptr, n_pages, page_size, scale,
+                          window, n_sink, out, row_max, row_sum, workspace, workspace_bytes, stream);
+}
+
+int antkv_qpage_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t qs_h, int64_t T, const int32_t* q_start, const int32_t* ctx_len,
+                     const int32_t* table, int64_t table_cap, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                     int64_t n_pages, int32_t page_size, float scale, int64_t window, int64_t n_sink, void* out, float* row_max, float* row_sum,
+                     void* workspace, size_t workspace_bytes, void* stream)
+{
+    return page_attn_impl(geom, q, qs_t, qs_h, T, q_start, ctx_len, table, table_cap, k_pages, v_pages, true, k_scales, v_scales, n_pages, page_size, scale,
+                          window, n_sink, out, row_max, row_sum, workspace, workspace_bytes, stream);
+}
+
+int antkv_rope_freqs(int32_t rot_dim, double base, double factor, double trained_len, double slow_turns, double fast_turns, double* freqs, void* stream)
+{
+    if (bad_rot(rot_dim)) return rot_dim < 2 || rot_dim > kD || (rot_dim & 1) ? ANTKV_EINVAL : ANTKV_EUNSUPPORTED;
+    const double most = 1e30;
+    if (!(base > 1.0 && base <= most) || !(factor > 0.0 && factor <= most) || !(trained_len >= 0.0 && trained_len <= most)) return ANTKV_EINVAL;
+    if (trained_len > 0.0 && !(slow_turns >= 0.0 && fast_turns > slow_turns && fast_turns <= most)) return ANTKV_EINVAL;
+    if (!freqs || misaligned(freqs, 8)) return ANTKV_EINVAL;
+    const hipError_t e = launch_rope_freqs(rot_dim, base, factor, trained_len, slow_turns, fast_turns, freqs, (hipStream_t)stream);
+    return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+}
+
+int antkv_rope(const antkv_geom* geom, const void* q, int64_t qs_b, int64_t qs_t, int64_t qs_h, const void* k, int64_t ks_b, int64_t ks_t, int64_t ks_h,
+               int64_t T, const int32_t* pos, const int32_t* q_start, const int32_t* ctx_len, int64_t pos0, const double* freqs, int32_t rot_dim,
+               int32_t rope_style, float amplitude, int32_t inverse, void* q_out, int64_t qo_b, int64_t qo_t, int64_t qo_h, void* k_out, int64_t ko_b,
+               int64_t ko_t, int64_t ko_h, void* stream)
+{
+    Geom g;
+    const int rc = check_geom(geom, g, kMostPagedPairs);
+    if (rc) return rc;
+    if (bad_rot(rot_dim)) return rot_dim < 2 || rot_dim > kD || (rot_dim & 1) ? ANTKV_EINVAL : ANTKV_EUNSUPPORTED;
+    if (rope_style != 0 && rope_style != 1) return ANTKV_EINVAL;
+    if ((q_start == nullptr) != (ctx_len == nullptr) || (q_start && pos) || pos0 < 0 || pos0 > 1LL << 40 || !(fabsf(amplitude) < INFINITY)) return ANTKV_EINVAL;
+    if (q_start && g.B > kMapRequests) return ANTKV_EUNSUPPORTED;
+    RopeArgs a;
+    a.B = q_start ? 1 : g.B;
+    a.R = g.B;
+    if (T < 0 || T > 0x7fffffffLL || a.B * T > 0x7fffffffLL) return ANTKV_EINVAL;
+    if (T == 0 || g.B == 0) return ANTKV_OK;
+    if ((!q && !k) || (q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || !freqs || misaligned(freqs, 8)) return ANTKV_EINVAL;
+    a.Hq = q ? g.Hq : 0;
+    a.Hkv = k ? g.Hkv : 0;
+    a.q = {(const half_t*)q, (half_t*)q_out, qs_b, qs_t, qs_h, qo_b, qo_t, qo_h};
+    a.k = {(const half_t*)k, (half_t*)k_out, ks_b, ks_t, ks_h, ko_b, ko_t, ko_h};
+    if ((q && bad_rope_rows(a.q, a.B, T, g.Hq)) || (k && bad_rope_rows(a.k, a.B, T, g.Hkv)) || (q && k && (q_out == k_out || q_out == k || k_out == q)))
+        return ANTKV_EINVAL;
+    a.T = T;
+    a.pos = pos; a.q_start = q_start; a.ctx_len = ctx_len; a.pos0 = pos0;
+    a.freqs = freqs; a.rot = rot_dim; a.style = rope_style; a.inverse = inverse != 0; a.amplitude = amplitude;
+    return launch_rope(a, (hipStream_t)stream) == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+}
+
+int antkv_qpage_store(const antkv_geom* geom, const void* k, const void* v, int64_t xs_t, int64_t xs_h, int64_t T, const int32_t* slot, void* k_pages,
+                      void* v_pages, float* k_scales, float* v_scales, int64_t n_pages, int32_t page_size, void* stream)
+{
+    Geom g;
+    int rc = check_geom(geom, g, kMostPagedPairs);
+    if (rc) return rc;
+    Pages pg;
+    rc = check_pages(n_pages, page_size, pg);
+    if (rc) return rc;
+    if (T < 0 || T > 0x7fffffffLL || (T + 15) / 16 * ((g.Hkv + 1) / 2) > kMostBlocks) return ANTKV_EINVAL;      // (a workgroup has 16 rows of two heads)
+    if (T == 0) return ANTKV_OK;
+    if (!k || !v || !slot || !k_pages || !v_pages || k_pages == v_pages || !k_scales || !v_scales || k_scales == v_scales) return ANTKV_EINVAL;
+    if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16) || misaligned(k_scales, 4) || misaligned(v_scales, 4)) return ANTKV_EINVAL;
+    if ((xs_t & 7) || (xs_h & 7) || xs_t < 0 || xs_h < 0) return ANTKV_EINVAL;
+    const hipError_t e = launch_qpage_store(g.Hkv, pg, (const half_t*)k, (const half_t*)v, xs_t, xs_h, T, slot, (uint8_t*)k_pages, (uint8_t*)v_pages, k_scales,
+                                            v_scales, (hipStream_t)stream);
+    return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
+}
+
+int antkv_qpage_load(const antkv_geom* geom, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales, int64_t n_pages,
+                     int32_t page_size, const int32_t* table, int64_t table_cap, const int32_t* ctx_len, int64_t first, int64_t N, void* k, void* v,
+                     int64_t xs_b, int64_t xs_h, int64_t xs_t, void* stream)
+{
+    Geom g;
+    int rc = check_geom(geom, g, kMostPagedPairs);
+    if (rc) return rc;
+    Pages pg;
+    rc = check_pages(n_pages, page_size, pg);
+    if (rc) return rc;
+    if (bad_table(table_cap, pg) || first < 0 || N < 0 || first > table_cap << pg.shift || N > (table_cap << pg.shift) - first) return ANTKV_EINVAL;
+    if (N == 0 || g.B == 0) return ANTKV_OK;
+    if (!k_pages || !v_pages || !k_scales || !v_scales || !table || !k || !v || k == v) return ANTKV_EINVAL;
+    if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16) || misaligned(k_scales, 4) || misaligned(v_scales, 4)) return ANTKV_EINVAL;
+    if (xs_t < kD || (xs_b & 7) || (xs_h & 7) || (xs_t & 7) || xs_b < 0 || xs_h < 0) return ANTKV_EINVAL;
+    const hipError_t e = launch_qpage_load(g.B, g.Hkv, pg, (const uint8_t*)k_pages, (const uint8_t*)v_pages, k_scales, v_scales, table, table_cap, ctx_len, first,
+                                           N, (half_t*)k, (half_t*)v, xs_b, xs_h, xs_t, (hipStream_t)stream);
+    return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
 }
 
 int antkv_anchor_select(const antkv_geom* geom, const void* q, const void* k_fp16, int64_t N, int64_t Nq, float scale,

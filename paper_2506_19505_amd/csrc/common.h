@@ -110,6 +110,10 @@ __device__ __forceinline__ uint32_t float_key(float f)
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 
+// Two fp16 values: which of them are not finite (their sign bits set), and the two without those.
+__device__ __forceinline__ uint32_t not_finite(uint32_t two) { return ((two & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t without(uint32_t two, uint32_t odd) { return two & ~((odd & 0x8000u ? 0xffffu : 0u) | (odd & 0x80000000u ? 0xffff0000u : 0u)); }
+
 // ---- launchers (each enqueues on `stream` and returns a hipError_t) --------------------------
 struct Geom {
     int B, Hq, Hkv, G, d, M;
@@ -191,9 +195,40 @@ struct PageAttnArgs {
     int window, n_sink;                                             // window 0: every earlier key is visible
     half_t* out;
     float *row_max, *row_sum;
+    const float *k_scales = nullptr, *v_scales = nullptr;           // pages of 8 bits
 };
 size_t page_attn_workspace_bytes(const Geom& g, int64_t T);
 hipError_t launch_page_attn(const Geom& g, const Pages& pg, const PageAttnArgs& a, void* ws, hipStream_t st);
+// q or k of a call on rotary positions: [B][T][heads][D] with strides in elements, channel stride 1
+struct RopeRows {
+    const half_t* x;
+    half_t* y;
+    int64_t xs_b, xs_t, xs_h, ys_b, ys_t, ys_h;
+};
+struct RopeArgs {
+    RopeRows q, k;
+    int64_t B, T;
+    int Hq, Hkv;                                                    // 0: none of them
+    const int32_t* pos;                                             // [B][T], or
+    const int32_t *q_start, *ctx_len;                               // of R requests in a packed batch (B = 1), or
+    int R;
+    int64_t pos0;                                                   // positions pos0, pos0 + 1, ..
+    const double* freqs;
+    int rot, style, inverse;
+    float amplitude;
+};
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st);
+hipError_t launch_rope_freqs(int rot, double base, double factor, double trained, double slow, double fast, double* freqs, hipStream_t st);
+
+// pages of 8 bits (bytes.h)
+hipError_t launch_qpage_store(int Hkv, const Pages& pg, const half_t* k, const half_t* v, int64_t xs_t, int64_t xs_h, int64_t T, const int32_t* slot,
+                              uint8_t* k_pages, uint8_t* v_pages, float* k_scales, float* v_scales, hipStream_t st);
+hipError_t launch_qpage_load(int B, int Hkv, const Pages& pg, const uint8_t* k_pages, const uint8_t* v_pages, const float* k_scales, const float* v_scales,
+                             const int32_t* table, int64_t table_cap, const int32_t* ctx_len, int64_t first, int64_t N, half_t* k, half_t* v, int64_t xs_b,
+                             int64_t xs_h, int64_t xs_t, hipStream_t st);
+// (k_pages and v_pages of the arguments are bytes)
+size_t qpage_attn_workspace_bytes(const Geom& g, int64_t T);
+hipError_t launch_qpage_attn(const Geom& g, const Pages& pg, const PageAttnArgs& a, void* ws, hipStream_t st);
 hipError_t launch_prefill_attn_window(const Geom& g, const half_t* q, const half_t* k, const half_t* v, int64_t N, int64_t Nq, float scale,
                                       int window, int n_sink, half_t* out, float* row_max, float* row_sum, hipStream_t st);
 

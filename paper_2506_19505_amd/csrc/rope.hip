@@ -1,0 +1,171 @@
+// Rotary positions: pairs of channels turned by the position times a frequency.
+//
+//   y_a = amplitude (x_a cos - x_b sin),  y_b = amplitude (x_b cos + x_a sin),  angle = position x freqs[i]  (inverse: the negative angle)
+//
+// of pair i = 0 .. rot / 2 - 1: channels (2 i, 2 i + 1) in style 0, (i, i + rot / 2) in style 1; channels from rot on are copied.
+//
+// A workgroup takes a few tokens with all of their heads.  A wave works out a token's 64 angles, one to a lane: the product with the position
+// and its reduction to a turn in fp64 (far positions turn thousands of times: fp32 would leave an error of 0.01 at 10^5), then sine and cosine
+// in fp32, and leaves them in LDS.  A thread turns 16 channels (eight pairs) of a head: 32 bytes in, 32 out, fp32 in between, rounded once.
+// Bound: HBM in long batches, launch and two dependent loads in short ones.
+#include "common.h"
+
+namespace antkv {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnits = kD / 16;                                     // threads of a head's row
+constexpr int kPass = kThreads / kUnits;                            // rows of a pass
+constexpr int kAhead = 4;                                           // passes whose loads are in flight together
+constexpr int kTokens = 16;                                         // of a workgroup, at most
+constexpr int kMostGroups = 1 << 20;
+constexpr double kTurn = 0.15915494309189533576888376337251;        // 1 / (2 pi)
+
+// The request whose rows hold row t: the last r < R with q_start[r] <= t (64 looked at at a time)
+__device__ __forceinline__ int request_at(const int32_t* q_start, int R, int64_t t, int lane)
+{
+    int lo = 0, n = R;
+    while (n > 1) {
+        const int step = (n + 63) / 64, at = lane * step;
+        const bool here = lane == 0 || (at < n && q_start[lo + (at < n ? at : 0)] <= t);
+        const int c = __builtin_popcountll(__ballot(here)) - 1;
+        lo += c * step;
+        n = n - c * step < step ? n - c * step : step;
+    }
+    return lo;
+}
+
+__global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs p, int tokens, int64_t groups)
+{
+    __shared__ float2_t s_turn[kTokens][kD / 2];                    // cosine, sine
+    __shared__ int s_seq[kTokens], s_tok[kTokens];                  // -1: nobody's row
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int H = p.Hq + p.Hkv, unit = tid % kUnits, pairs = p.rot / 2;
+    const int half = p.rot / 16;                                    // 16-byte pieces between the channels of a pair, style 1
+    // the unit's two 16-byte pieces
+    const bool turns = 16 * unit < p.rot;
+    const int a = p.style == 1 && turns ? unit : 2 * unit, b = p.style == 1 && turns ? unit + half : 2 * unit + 1;
+    for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
+        const int64_t first = group * tokens;                       // token of all B x T
+        if (group != blockIdx.x) __syncthreads();
+        for (int i = wave; i < tokens; i += kThreads / 64) {
+            const int64_t u = first + i;
+            bool live = u < p.B * p.T;
+            int64_t pos = 0;
+            if (live && p.q_start) {
+                const int r = request_at(p.q_start, p.R, u, lane);
+                const int64_t from = p.q_start[r], end = p.q_start[r + 1];
+                live = u >= from && u < end;
+                pos = p.ctx_len[r] - end + u;
+            } else if (live) {
+                pos = p.pos ? p.pos[u] : p.pos0 + u % p.T;
+            }
+            if (live && lane < pairs) {
+                const double turn = (double)pos * p.freqs[lane] * kTurn;
+                float s, c;
+                sincospif(2.f * (float)(turn - rint(turn)), &s, &c);
+                s_turn[i][lane] = float2_t{c * p.amplitude, s * (p.inverse ? -p.amplitude : p.amplitude)};
+            }
+            if (lane == 0) {
+                const int64_t n = p.B > 1 && live ? u / p.T : 0;
+                s_seq[i] = live ? (int)n : -1;
+                s_tok[i] = (int)(u - n * p.T);
+            }
+        }
+        __syncthreads();
+        const int rows = tokens * H;
+        for (int row0 = tid / kUnits; row0 < rows; row0 += kAhead * kPass) {
+            uint4_t x[kAhead], y[kAhead];
+            uint4_t* to[kAhead];
+            int at[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int row = row0 + j * kPass;
+                to[j] = nullptr;
+                if (row < rows) {
+                    const int i = row / H, h = row - i * H;
+                    const int64_t n = s_seq[i], t = s_tok[i];
+                    if (n >= 0) {
+                        const RopeRows& z = h < p.Hq ? p.q : p.k;
+                        const int hh = h < p.Hq ? h : h - p.Hq;
+                        const uint4_t* from = (const uint4_t*)(z.x + n * z.xs_b + t * z.xs_t + hh * z.xs_h);
+                        to[j] = (uint4_t*)(z.y + n * z.ys_b + t * z.ys_t + hh * z.ys_h);
+                        x[j] = from[a];
+                        y[j] = from[b];
+                        at[j] = i;
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (to[j]) {
+                    if (turns) {
+                        const float4_t* cs = (const float4_t*)&s_turn[at[j]][8 * unit];
+                        float c[8], s[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            c[e] = cs[e >> 1][2 * (e & 1)];
+                            s[e] = cs[e >> 1][2 * (e & 1) + 1];
+                        }
+                        half8_t u = __builtin_bit_cast(half8_t, x[j]), w = __builtin_bit_cast(half8_t, y[j]), yu, yw;
+                        if (p.style == 1) {                         // pair e: channel e of either piece
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                yu[e] = (half_t)((float)u[e] * c[e] - (float)w[e] * s[e]);
+                                yw[e] = (half_t)((float)w[e] * c[e] + (float)u[e] * s[e]);
+                            }
+                        } else {                                    // pair e: channels 2 e, 2 e + 1 of the sixteen
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                yu[2 * e] = (half_t)((float)u[2 * e] * c[e] - (float)u[2 * e + 1] * s[e]);
+                                yu[2 * e + 1] = (half_t)((float)u[2 * e + 1] * c[e] + (float)u[2 * e] * s[e]);
+                                yw[2 * e] = (half_t)((float)w[2 * e] * c[4 + e] - (float)w[2 * e + 1] * s[4 + e]);
+                                yw[2 * e + 1] = (half_t)((float)w[2 * e + 1] * c[4 + e] + (float)w[2 * e] * s[4 + e]);
+                            }
+                        }
+                        x[j] = __builtin_bit_cast(uint4_t, yu);
+                        y[j] = __builtin_bit_cast(uint4_t, yw);
+                    }
+                    to[j][a] = x[j];
+                    to[j][b] = y[j];
+                }
+        }
+    }
+}
+
+__global__ void rope_freqs_kernel(int rot, double base, double factor, double trained, double slow, double fast, double* freqs)
+{
+    const int i = threadIdx.x;
+    if (i >= rot / 2) return;
+    const double f = pow(base, -2.0 * i / rot);
+    double w = 0.0;                                                 // share of the frequency that stays
+    if (trained > 0.0) {
+        w = (trained * f * kTurn - slow) / (fast - slow);
+        w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
+    }
+    freqs[i] = f * (w + (1.0 - w) / factor);
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st)
+{
+    const int H = a.Hq + a.Hkv;
+    const int64_t all = a.B * a.T;
+    // a workgroup's tokens: all of its passes in flight at once, where that leaves a workgroup for every CU
+    int tokens = kAhead * kPass / H;
+    tokens = tokens < 1 ? 1 : tokens < kTokens ? tokens : kTokens;
+    while (tokens > 1 && all / tokens < 1024) tokens /= 2;
+    const int64_t groups = (all + tokens - 1) / tokens;
+    hipLaunchKernelGGL(rope_kernel, dim3((unsigned)(groups < kMostGroups ? groups : kMostGroups)), dim3(kThreads), 0, st, a, tokens, groups);
+    return hipGetLastError();
+}
+
+hipError_t launch_rope_freqs(int rot, double base, double factor, double trained, double slow, double fast, double* freqs, hipStream_t st)
+{
+    hipLaunchKernelGGL(rope_freqs_kernel, dim3(1), dim3(kD / 2), 0, st, rot, base, factor, trained, slow, fast, freqs);
+    return hipGetLastError();
+}
+
+}  // namespace antkv

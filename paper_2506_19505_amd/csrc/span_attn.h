@@ -38,6 +38,7 @@ constexpr int kRing = 4;                                // tiles of K, and of V,
 constexpr int kRingBytes = 2 * kRing * kTileBytes;
 constexpr int kTurn = 512;                              // key tiles that are looked up at a time
 constexpr int kNotes = kTurn + 8;                       // and what lies behind them: see Note
+constexpr int kByteNotes = kTurn + 12;                  // of pages of 8 bits
 constexpr float kPMax = 15.f, kLift = 8.f;
 constexpr float kMasked = -INFINITY;                    // a score that takes no part
 
@@ -60,6 +61,7 @@ struct Params {
     unsigned long long* done;                                       // [shares][Hkv] arrival words (launch_tag.h) of the blocks that end there
     uint64_t tag;
     float *part_out, *part_stat;                                    // [2 shares][Hkv][rows_cap] x D sums, x 4: reference, sum, largest score
+    const float *k_scales, *v_scales;                               // pages of 8 bits: of every 16 tokens of a head
 };
 
 __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }      // of a value that is the same in every lane
@@ -241,13 +243,10 @@ struct Operands {
     }
 };
 
-// Two fp16 values of V: which of them are not finite (their sign bits set), and the two without those.
-__device__ __forceinline__ uint32_t not_finite(uint32_t two) { return ((two & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
-__device__ __forceinline__ uint32_t without(uint32_t two, uint32_t odd) { return two & ~((odd & 0x8000u ? 0xffffu : 0u) | (odd & 0x80000000u ? 0xffff0000u : 0u)); }
-
 // Values of a V tile that are not finite, as inf, -inf or NaN to the rows that see them: each row's number of them per channel is a
 // matrix product of its own, in which fp16 1 stands for inf, 64 for -inf and 4096 for NaN (sums of 32 keep apart).
-__device__ __forceinline__ void add_odd(Sums& x, const Operands& at, int slot, uint32_t seen)
+template <class At>
+__device__ __forceinline__ void add_odd(Sums& x, const At& at, int slot, uint32_t seen)
 {
 #pragma unroll
     for (int cg = 0; cg < 4; ++cg) {
@@ -281,15 +280,52 @@ __device__ __forceinline__ void add_odd(Sums& x, const Operands& at, int slot, u
     }
 }
 
-// The query row of each lane (row n of the tile that starts at row w_row; rows behind the last repeat it)
+// The query row of each lane (row n of the tile that starts at row w_row; rows behind the last repeat it).  k-step s takes channels 16 s + 8 kh
+// .. + 7; kPairs: 32 (s / 2) + 16 kh + 8 (s % 2) .. + 7, so that two steps of an operand of K are 16 channels in a row
+template <bool kPairs = false>
 __device__ __forceinline__ void load_query(half8_t (&tq)[8], const Params& p, const Piece& x, int row, int lane)
 {
     const int tok = row >> p.gs, h = (x.g << p.gs) + (row & (p.G - 1));
-    const half_t* qp = p.q + x.b * p.qs_b + (int64_t)(x.rq.t0 + tok) * p.qs_t + h * p.qs_h + 8 * (lane >> 5);
+    const half_t* qp = p.q + x.b * p.qs_b + (int64_t)(x.rq.t0 + tok) * p.qs_t + h * p.qs_h + (kPairs ? 16 : 8) * (lane >> 5);
 #pragma unroll
-    for (int s = 0; s < 8; ++s) tq[s] = *(const half8_t*)(qp + 16 * s);
+    for (int s = 0; s < 8; ++s) tq[s] = *(const half8_t*)(qp + (kPairs ? 32 * (s >> 1) + 8 * (s & 1) : 16 * s));
 #pragma unroll
     for (int s = 0; s < 8; ++s) pin(tq[s]);
+}
+
+// Softmax of a tile's scores s, whose probabilities are then in `now`, with the scores y of the tile in K slot `next` and the value product of
+// the one in V slot `prev`, of probabilities `before`: neither matrix product waits for the other or for the softmax.  under(j): what else
+// the wave does beside the jth pair of them.
+template <class Under>
+__device__ __forceinline__ void tile_step(Sums& sums, const Operands& at, const half8_t (&tq)[8], float c1, int next, int prev, const float16_t& s, float16_t& y,
+                                          half8_t (&now)[2], const half8_t (&before)[2], const Under& under)
+{
+    float alpha;
+    const bool moves = sums.open(s, c1, alpha);
+    half8_t ka[8], va[8];
+    ka[0] = at.k_op(0, next); va[0] = at.v_op(0, prev);
+    ka[1] = at.k_op(1, next); va[1] = at.v_op(1, prev);
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) y[r] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (j + 2 < 8) { ka[j + 2] = at.k_op(j + 2, next); va[j + 2] = at.v_op(j + 2, prev); }
+        y = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[j], tq[j], y, 0, 0, 0);                               // rows = keys, cols = queries
+        float p0 = fast_exp2(fmaf(s[2 * j], c1, -sums.m_ref));
+        sum[0] += p0;
+        sums.o[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va[j], before[j >> 2], sums.o[j & 3], 0, 0, 0);   // rows = channels
+        float p1 = fast_exp2(fmaf(s[2 * j + 1], c1, -sums.m_ref));
+        sum[1] += p1;
+        pin(sum[0]);                                        // (the products must not sink below the loop)
+        pin(sum[1]);
+        now[j >> 2][(2 * j) & 7] = (half_t)p0;
+        now[j >> 2][(2 * j + 1) & 7] = (half_t)p1;
+        under(j);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    sums.l += sum[0] + sum[1];
+    if (__builtin_expect(moves, 0)) sums.rescale(alpha);
 }
 
 // What the loop has to know of a key tile, looked up for a whole turn at once.  Behind the turn's last tile follow copies of it
@@ -297,7 +333,7 @@ __device__ __forceinline__ void load_query(half8_t (&tq)[8], const Params& p, co
 struct Note {
     int place[2];                                                   // of its 16-key halves, in 16 keys of a head, x 4; bits 0: the context's last tile, 1: no page
     int edge;                                                       // bit w: some row of wave w does not see some key, kEdgeAny: some row of the workgroup, kHidden: nobody sees any
-    int unused;
+    int exponents;                                                  // pages of 8 bits: of the scales of K, first and second half, and of V
 };
 constexpr int kLast = 1, kBad = 2, kEdgeAny = 1 << 8, kHidden = 1 << 9;
 
@@ -382,7 +418,7 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
                 for (int w = 0; w < NW; ++w)
                     if (bad || !sight.whole(tile, sees_to(x.row0 + 32 * w), stands_at(x.row0 + 32 * w + 31))) note.edge |= 1 << w;
             }
-            note.unused = 0;
+            note.exponents = 0;
             notes[i] = note;
         }
         // the V slot of "tile -1" is multiplied with zero probabilities: it has to be finite
@@ -475,31 +511,7 @@ __device__ __forceinline__ void wide_sums(Sums& sums, const Params& p, const Pie
             const int next = (T + 1) & 3, prev = (T + 3) & 3;
             const uint32_t edge = stage_ahead(i, T);
             if (__builtin_expect(edge & 1, 0)) mask(s, seen_of(i));
-            float alpha;
-            const bool moves = sums.open(s, p.c1, alpha);
-            half8_t ka[8], va[8];
-            ka[0] = at.k_op(0, next); va[0] = at.v_op(0, prev);
-            ka[1] = at.k_op(1, next); va[1] = at.v_op(1, prev);
-            float sum[2] = {0.f, 0.f};
-#pragma unroll
-            for (int r = 0; r < 16; ++r) y[r] = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (j + 2 < 8) { ka[j + 2] = at.k_op(j + 2, next); va[j + 2] = at.v_op(j + 2, prev); }
-                y = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[j], tq[j], y, 0, 0, 0);                               // rows = keys, cols = queries
-                float p0 = fast_exp2(fmaf(s[2 * j], p.c1, -sums.m_ref));
-                sum[0] += p0;
-                sums.o[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(va[j], before[j >> 2], sums.o[j & 3], 0, 0, 0);   // rows = channels
-                float p1 = fast_exp2(fmaf(s[2 * j + 1], p.c1, -sums.m_ref));
-                sum[1] += p1;
-                pin(sum[0]);                                        // (the products must not sink below the loop)
-                pin(sum[1]);
-                now[j >> 2][(2 * j) & 7] = (half_t)p0;
-                now[j >> 2][(2 * j + 1) & 7] = (half_t)p1;
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            sums.l += sum[0] + sum[1];
-            if (__builtin_expect(moves, 0)) sums.rescale(alpha);
+            tile_step(sums, at, tq, p.c1, next, prev, s, y, now, before, [](int) {});
             land(T, edge);
         };
         if (active) {
