@@ -383,8 +383,9 @@ int antkv_page_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t
  *   most, 2^-9 s over all times).  So positions of a request have to come in order, as antkv_page_map hands out their slots; a request that is cut back may
  *   go on from any position.
  *   The rows of a block lie within 16 rows of the batch that follow each other, in any order (positions in order do, also with some left out); slots of one call are
- *   distinct.  A block whose rows lie further apart, or a slot given twice, leaves that block with undefined values.  The grid sets the limit of T: ceil(T / 16) * ceil(Hkv / 2) below 2^24.
- * antkv_qpage_load is antkv_page_load: fp16 rows out.
+ *   distinct.  A block whose rows lie further apart, or a slot given twice, leaves that block with undefined values.  The grid sets the limit of T: ceil(T / 16) * ceil(Hkv / 4) below 2^24.
+ * antkv_qpage_load is antkv_page_load: fp16 rows out.  With clear != 0 rows at or behind ctx_len[b] and rows of pages that are none become zeros
+ * instead of being left as they are.
  * antkv_qpage_attn is antkv_page_attn over the values that antkv_qpage_load would give, to the same precision; its workspace size comes from
  * antkv_qpage_attn_workspace.
  * Scales that antkv_qpage_store has not made: antkv_qpage_load and antkv_qpage_attn take a positive normal number for the power of two at or below it; a block that goes
@@ -394,7 +395,7 @@ int antkv_qpage_store(const antkv_geom* geom, const void* k, const void* v, int6
                       void* v_pages, float* k_scales, float* v_scales, int64_t n_pages, int32_t page_size, void* stream);
 int antkv_qpage_load(const antkv_geom* geom, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales, int64_t n_pages,
                      int32_t page_size, const int32_t* table, int64_t table_cap, const int32_t* ctx_len, int64_t first, int64_t N, void* k, void* v,
-                     int64_t xs_b, int64_t xs_h, int64_t xs_t, void* stream);
+                     int64_t xs_b, int64_t xs_h, int64_t xs_t, int32_t clear, void* stream);
 size_t antkv_qpage_attn_workspace(const antkv_geom* geom, int64_t T);
 int antkv_qpage_attn(const antkv_geom* geom, const void* q, int64_t qs_t, int64_t qs_h, int64_t T, const int32_t* q_start, const int32_t* ctx_len,
                      const int32_t* table, int64_t table_cap, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,

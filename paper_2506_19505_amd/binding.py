@@ -125,7 +125,7 @@ def load_library():
         lib.antkv_qpage_store.restype = ctypes.c_int
         lib.antkv_qpage_store.argtypes = [gp, vp, vp, i64, i64, i64, vp, vp, vp, vp, vp, i64, i32, vp]
         lib.antkv_qpage_load.restype = ctypes.c_int
-        lib.antkv_qpage_load.argtypes = [gp, vp, vp, vp, vp, i64, i32, vp, i64, vp, i64, i64, vp, vp, i64, i64, i64, vp]
+        lib.antkv_qpage_load.argtypes = [gp, vp, vp, vp, vp, i64, i32, vp, i64, vp, i64, i64, vp, vp, i64, i64, i64, i32, vp]
         lib.antkv_qpage_attn_workspace.restype = sz
         lib.antkv_qpage_attn_workspace.argtypes = [gp, i64]
         lib.antkv_qpage_attn.restype = ctypes.c_int
@@ -653,18 +653,22 @@ def qpage_load(geom: Geometry, k_pages: torch.Tensor, v_pages: torch.Tensor, k_s
     if ctx_len is not None:
         _ints(ctx_len, "ctx_len", (geom.B,))
     shape = (geom.B, geom.Hkv, N, geom.D)
-    if k is None:
-        k = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
-    if v is None:
-        v = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
-    _need(k, torch.float16, "k")
-    _need(v, torch.float16, "v")
-    if k.shape != shape or v.shape != shape:
-        raise ValueError(f"k and v must be {list(shape)}")
+    clear = k is None and v is None
+    if clear:
+        k, v = k_scales.new_empty((2, *shape), dtype=torch.float16).unbind(0)
+    else:
+        if k is None:
+            k = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
+        if v is None:
+            v = torch.zeros(shape, dtype=torch.float16, device=k_pages.device)
+        _need(k, torch.float16, "k")
+        _need(v, torch.float16, "v")
+        if k.shape != shape or v.shape != shape:
+            raise ValueError(f"k and v must be {list(shape)}")
     rows = N * geom.D
     _run(load_library().antkv_qpage_load, "antkv_qpage_load", _one_device(k_pages, v_pages, k_scales, v_scales, table, ctx_len, k, v), geom._c,
          k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n_pages, page_size, table.data_ptr(), cap, _p(ctx_len), first, N,
-         k.data_ptr(), v.data_ptr(), geom.Hkv * rows, rows, geom.D, _stream(k_pages))
+         k.data_ptr(), v.data_ptr(), geom.Hkv * rows, rows, geom.D, clear, _stream(k_pages))
     return k, v
 
 
@@ -723,28 +727,36 @@ def rope_freqs(rot_dim: int = 128, base: float = 10000.0, factor: float = 1.0, t
 
 
 def _rope_rows(x: torch.Tensor, out: torch.Tensor | None, name: str, heads: int, batch: int, packed: bool):
-    """x fp16 [T,heads,D] (packed, or one sequence) or [B,heads,T,D], channels contiguous -> (T, out, strides b, t, h of both)."""
+    """x fp16 [T,heads,D] (packed, or one sequence) or [B,heads,T,D], channels contiguous -> (T, out, strides b, t, h of x, of out)."""
+    shape = x.shape
+    if len(shape) == 3:
+        T, h, d = shape
+        fits = packed or batch == 1
+    elif len(shape) == 4:
+        b, h, T, d = shape
+        fits = b == batch and not packed
+    else:
+        fits = False
     if not x.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if x.dtype is not torch.float16:
         raise TypeError(f"{name} must be torch.float16")
-    shape, d = x.shape, x.dim()
-    if d == 3 and (packed or batch == 1):
-        T, fits = shape[0], shape[1:] == (heads, 128)
-    elif d == 4 and not packed:
-        T, fits = shape[2], (shape[0], shape[1], shape[3]) == (batch, heads, 128)
-    else:
-        fits = False
-    if not fits or x.stride(-1) != 1:
-        raise ValueError(f"{name} must be " + (f"[T, {heads}, 128]" if packed else f"[{batch}, {heads}, T, 128]" + (f" or [T, {heads}, 128]" if batch == 1 else "")) +
-                         " with contiguous channels")
+    a = x.stride()
+    if not fits or h != heads or d != 128 or a[-1] != 1:
+        raise ValueError(f"{name} must be [T, {heads}, 128] of a packed batch or of one sequence, or [{batch}, {heads}, T, 128], with contiguous channels")
     if out is None:
-        out = torch.empty(shape, dtype=torch.float16, device=x.device)
-    elif out is not x:
-        if out.get_device() != x.get_device() or out.dtype is not torch.float16 or out.shape != shape or out.stride(-1) != 1:
+        out = x.new_empty(shape)
+        o = out.stride()
+    else:
+        o = out.stride()
+        if out is not x and (out.get_device() != x.get_device() or out.dtype is not torch.float16 or out.shape != shape or o[-1] != 1):
             raise ValueError(f"{name}_out must be like {name}")
-    a, b = x.stride(), out.stride()
-    return T, out, (0, a[0], a[1]) if d == 3 else (a[0], a[2], a[1]), (0, b[0], b[1]) if d == 3 else (b[0], b[2], b[1])
+    if len(a) == 3:
+        return T, out, x.data_ptr(), 0, a[0], a[1], out.data_ptr(), 0, o[0], o[1]
+    return T, out, x.data_ptr(), a[0], a[2], a[1], out.data_ptr(), o[0], o[2], o[1]
+
+
+_NO_ROWS = None, None, None, 0, 0, 0, None, 0, 0, 0
 
 
 def rope(geom: Geometry, q: torch.Tensor | None, k: torch.Tensor | None, freqs: torch.Tensor, pos: torch.Tensor | None = None,
@@ -758,20 +770,14 @@ def rope(geom: Geometry, q: torch.Tensor | None, k: torch.Tensor | None, freqs: 
     _need(freqs, torch.float64, "freqs")
     if freqs.dim() != 1:
         raise ValueError("freqs must be [rot_dim / 2]")
-    first = q if q is not None else k
+    first = k if q is None else q
     if first is None:
         raise ValueError("q or k must be given")
-    T, none = None, (None, (0, 0, 0), (0, 0, 0))
-    rows = []
-    for x, out, name, heads in ((q, q_out, "q", geom.Hq), (k, k_out, "k", geom.Hkv)):
-        if x is None:
-            rows.append(none)
-            continue
-        n, *row = _rope_rows(x, out, name, heads, geom.B, packed)
-        if T is not None and (n != T or x.dim() != first.dim()):
-            raise ValueError("q and k must have the same rows")
-        T = n
-        rows.append(row)
+    Tq, q_out, *qs = _NO_ROWS if q is None else _rope_rows(q, q_out, "q", geom.Hq, geom.B, packed)
+    Tk, k_out, *ks = _NO_ROWS if k is None else _rope_rows(k, k_out, "k", geom.Hkv, geom.B, packed)
+    T = Tk if q is None else Tq
+    if q is not None and k is not None and (Tq != Tk or q.dim() != k.dim()):
+        raise ValueError("q and k must have the same rows")
     if packed:
         _ints(q_start, "q_start", (geom.B + 1,))
         if ctx_len is None:
@@ -779,8 +785,6 @@ def rope(geom: Geometry, q: torch.Tensor | None, k: torch.Tensor | None, freqs: 
         _ints(ctx_len, "ctx_len", (geom.B,))
     if pos is not None:
         _ints(pos, "pos", (T,) if first.dim() == 3 else (geom.B, T))
-    (q_out, qs, qo), (k_out, ks, ko) = rows
-    _run(load_library().antkv_rope, "antkv_rope", _one_device(first, q, k, q_out, k_out, freqs, pos, q_start, ctx_len), geom._c, _p(q), *qs, _p(k), *ks, T,
-         _p(pos), _p(q_start), _p(ctx_len), int(pos0), freqs.data_ptr(), 2 * freqs.shape[0], int(style), float(amplitude), int(bool(inverse)), _p(q_out), *qo,
-         _p(k_out), *ko, _stream(first))
+    _run(load_library().antkv_rope, "antkv_rope", _one_device(first, q, k, freqs, pos, q_start, ctx_len), geom._c, *qs[:4], *ks[:4], T, _p(pos), _p(q_start),
+         _p(ctx_len), pos0, freqs.data_ptr(), 2 * freqs.shape[0], style, amplitude, inverse, *qs[4:], *ks[4:], _stream(first))
     return q_out, k_out

@@ -492,7 +492,7 @@ int antkv_qpage_store(const antkv_geom* geom, const void* k, const void* v, int6
     Pages pg;
     rc = check_pages(n_pages, page_size, pg);
     if (rc) return rc;
-    if (T < 0 || T > 0x7fffffffLL || (T + 15) / 16 * ((g.Hkv + 1) / 2) > kMostBlocks) return ANTKV_EINVAL;      // (a workgroup has 16 rows of two heads)
+    if (T < 0 || T > 0x7fffffffLL || (T + 15) / 16 * ((g.Hkv + 3) / 4) > kMostBlocks) return ANTKV_EINVAL;      // (a workgroup has 16 rows of four heads)
     if (T == 0) return ANTKV_OK;
     if (!k || !v || !slot || !k_pages || !v_pages || k_pages == v_pages || !k_scales || !v_scales || k_scales == v_scales) return ANTKV_EINVAL;
     if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16) || misaligned(k_scales, 4) || misaligned(v_scales, 4)) return ANTKV_EINVAL;
@@ -504,7 +504,7 @@ int antkv_qpage_store(const antkv_geom* geom, const void* k, const void* v, int6
 
 int antkv_qpage_load(const antkv_geom* geom, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales, int64_t n_pages,
                      int32_t page_size, const int32_t* table, int64_t table_cap, const int32_t* ctx_len, int64_t first, int64_t N, void* k, void* v,
-                     int64_t xs_b, int64_t xs_h, int64_t xs_t, void* stream)
+                     int64_t xs_b, int64_t xs_h, int64_t xs_t, int32_t clear, void* stream)
 {
     Geom g;
     int rc = check_geom(geom, g, kMostPagedPairs);
@@ -518,7 +518,7 @@ int antkv_qpage_load(const antkv_geom* geom, const void* k_pages, const void* v_
     if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16) || misaligned(k_scales, 4) || misaligned(v_scales, 4)) return ANTKV_EINVAL;
     if (xs_t < kD || (xs_b & 7) || (xs_h & 7) || (xs_t & 7) || xs_b < 0 || xs_h < 0) return ANTKV_EINVAL;
     const hipError_t e = launch_qpage_load(g.B, g.Hkv, pg, (const uint8_t*)k_pages, (const uint8_t*)v_pages, k_scales, v_scales, table, table_cap, ctx_len, first,
-                                           N, (half_t*)k, (half_t*)v, xs_b, xs_h, xs_t, (hipStream_t)stream);
+                                           N, (half_t*)k, (half_t*)v, xs_b, xs_h, xs_t, clear != 0, (hipStream_t)stream);
     return e == hipSuccess ? ANTKV_OK : ANTKV_ELAUNCH;
 }
 

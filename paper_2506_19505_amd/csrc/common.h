@@ -112,7 +112,8 @@ __device__ __forceinline__ uint32_t float_key(float f)
 
 // Two fp16 values: which of them are not finite (their sign bits set), and the two without those.
 __device__ __forceinline__ uint32_t not_finite(uint32_t two) { return ((two & 0x7c007c00u) + 0x04000400u) & 0x80008000u; }
-__device__ __forceinline__ uint32_t without(uint32_t two, uint32_t odd) { return two & ~((odd & 0x8000u ? 0xffffu : 0u) | (odd & 0x80000000u ? 0xffff0000u : 0u)); }
+// (a sign bit at 15 or 31 becomes the 16 bits up to it: 2^16 - 1, 2^32 - 2^16)
+__device__ __forceinline__ uint32_t without(uint32_t two, uint32_t odd) { return two & ~((odd << 1) - (odd >> 15)); }
 
 // ---- launchers (each enqueues on `stream` and returns a hipError_t) --------------------------
 struct Geom {
@@ -225,7 +226,7 @@ hipError_t launch_qpage_store(int Hkv, const Pages& pg, const half_t* k, const h
                               uint8_t* k_pages, uint8_t* v_pages, float* k_scales, float* v_scales, hipStream_t st);
 hipError_t launch_qpage_load(int B, int Hkv, const Pages& pg, const uint8_t* k_pages, const uint8_t* v_pages, const float* k_scales, const float* v_scales,
                              const int32_t* table, int64_t table_cap, const int32_t* ctx_len, int64_t first, int64_t N, half_t* k, half_t* v, int64_t xs_b,
-                             int64_t xs_h, int64_t xs_t, hipStream_t st);
+                             int64_t xs_h, int64_t xs_t, bool clear, hipStream_t st);
 // (k_pages and v_pages of the arguments are bytes)
 size_t qpage_attn_workspace_bytes(const Geom& g, int64_t T);
 hipError_t launch_qpage_attn(const Geom& g, const Pages& pg, const PageAttnArgs& a, void* ws, hipStream_t st);

@@ -57,10 +57,8 @@ struct Cost {
             if (p.window == 0 && q.p0 >= 0 && q.p0 + q.n <= q.limit) step = kRows / 32 >> p.gs;
         }
     }
-    // Key tiles' worth of coming and going: looking up pages, the first loads, partial sums.  Narrow 14, 20, 28: 16
-    // tokens on 300 keys each 11.0, 15.0, 16.2 us, 63 tokens beside one chunk of 100 on 2000 keys each 105, 106, 118, 64 on 1 .. 32768 keys 147, 148,
-    // 147 (4, measured earlier: 208 where 20 took 176).  Wide 12, 16, 20: 300 tokens on 2000 keys 46, 38, 46, 8 prompts of 1024 131, 121, 119
-    __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? 14 : 16; }
+    // key tiles' worth of coming and going: looking up pages, the first loads, partial sums
+    __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? Cache::kIdleNarrow : Cache::kIdleWide; }
     __device__ __forceinline__ int before(int k) const { return k * a - step * (k * (k - 1) / 2); }      // of blocks 0 .. k - 1
     __device__ __forceinline__ int all() const { return before(blocks); }
     __device__ __forceinline__ int block_at(int x) const            // the block in which x lies
@@ -281,9 +279,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
     int size = 1, x = share, end = total;                           // the share: costs x .. end - 1 (unit: block x)
     if (!p.unit) {
         size = (total + p.shares - 1) / p.shares;
-        // Less is not worth the partial sums.  8, 12, 16: a token on 4096 keys 14.7, 13.2, 13.8 us, one each of 4 requests on 2048 keys 16.6,
-        // 14.5, 14.9; 16, 24, 32: 64 tokens on 4096 keys 32.5, 33.9, 36.0, 300 on 2000 39.4, 38.1, 46.2, 4 x 100 on 1000 32.1, 31.4, 32.0
-        const int least = wide ? 24 : 12;
+        const int least = wide ? Cache::kLeastWide : Cache::kLeastNarrow;       // less is not worth the partial sums
         if (size < least) size = least;
         x = share < p.shares ? share * size : total;
         end = x + size < total ? x + size : total;
@@ -435,7 +431,8 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
 // The lengths are on the device, so that the host goes by the mean.  One long chunk among many short requests is on the slower side then, 2048 tokens on
 // 32768 keys beside 63 single tokens on 2000 each 1129 and 1185, beside 63 requests without a token 1018 and 1104; the same 63 beside 2048 tokens on
 // 4096 keys 220 and 192, beside 512 on 8192 183 and 149, 31 on 500 .. 16000 beside 2048 on 2048 275 and 219.
-inline int waves_of(const Geom& g, int64_t T) { return T * g.G >= (int64_t)g.B * 1024 ? 8 : 4; }
+template <class Cache>
+inline int waves_of(const Geom& g, int64_t T) { return T * g.G >= (int64_t)g.B * Cache::kRowsOfEight ? 8 : 4; }
 // Shares per KV head: the chip's workgroups, or one each.
 inline int shares_of(const Geom& g, int nw) { return g.Hkv < kWaves / nw ? kWaves / nw / g.Hkv : 1; }
 // A batch has no block of more rows than it has itself.
@@ -488,7 +485,7 @@ inline hipError_t launch(const Geom& g, const Pages& pg, const PageAttnArgs& a, 
     p.c1 = a.scale * kLog2e; p.Hkv = g.Hkv; p.G = g.G; p.gs = log2_of(g.G); p.window = a.window; p.n_sink = a.n_sink;
     p.q_start = a.q_start; p.ctx_len = a.ctx_len; p.table = a.table; p.table_cap = a.table_cap; p.n_pages = pg.n;
     p.T = (int)a.T; p.R = g.B; p.shift = pg.shift; p.k_scales = a.k_scales; p.v_scales = a.v_scales;
-    return waves_of(g, a.T) == 8 ? launch_waves<Cache, 8>(g, p, a.T, ws, st) : launch_waves<Cache, 4>(g, p, a.T, ws, st);
+    return waves_of<Cache>(g, a.T) == 8 ? launch_waves<Cache, 8>(g, p, a.T, ws, st) : launch_waves<Cache, 4>(g, p, a.T, ws, st);
 }
 
 }  // namespace paged

@@ -61,6 +61,16 @@ struct ByteOperands {
 };
 
 struct BytePages {
+    // As page_attn.hip's, measured again.  What a narrow block costs beside its tiles, 14, 16, 20: 64 tokens on 1 .. 32768 keys each 88.0, 85.2, 84.1 us, 128 on
+    // 1 .. 16384 113, 105, 111, 300 x 20 on 40 .. 1500 150, 144, 161, 16 on 300 each 11.6, 12.7, 13.2.  A wide one, 16 and 24: 300 tokens on 2000 keys 42 and 49, 8
+    // prompts of 1024 131 and 126, 64 tokens on 4096 38 and 42
+    static constexpr int kIdleNarrow = 16, kIdleWide = 16;
+    // The smallest shares.  12 and 18: a token on 4096 keys 12.5 and 13.5 us, one each of 4 requests on 2048 13.7 and 14.5; 24 and 36: 300 tokens on 2000 keys 42
+    // and 52
+    static constexpr int kLeastNarrow = 12, kLeastWide = 24;
+    // 1024 and 512: 16 requests with 2048 tokens among them 88 and 102 us; 1024 and 256: 64 tokens on 4096 keys 39 and 50
+    static constexpr int kRowsOfEight = 1024;
+
     template <int NW>                                   // waves of a workgroup: 8 or 4
     struct Lds {
         static constexpr int tiles = 0;                                 // narrow: two K and V tiles per wave; wide: the rings
@@ -396,8 +406,8 @@ struct BytePages {
                 take(i, T);
                 if (__builtin_expect(edge & 1, 0)) mask(s, seen_of(i));
                 tile_step(sums, at, tq, p.c1, (T + 1) & 1, (T + 1) & 1, s, y, now, before, [&](int j) __attribute__((always_inline)) {
-                    if (j == 3) make(0, T);
-                    if (kStreams > 1 && j == 5) make(1, T);
+                    if (j == (kStreams > 1 ? 4 : 3)) make(0, T);
+                    if (kStreams > 1 && j == 6) make(1, T);
                 });
                 end(i, T);
             };

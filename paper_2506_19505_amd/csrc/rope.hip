@@ -7,7 +7,7 @@
 // A workgroup takes a few tokens with all of their heads.  A wave works out a token's 64 angles, one to a lane: the product with the position
 // and its reduction to a turn in fp64 (far positions turn thousands of times: fp32 would leave an error of 0.01 at 10^5), then sine and cosine
 // in fp32, and leaves them in LDS.  A thread turns 16 channels (eight pairs) of a head: 32 bytes in, 32 out, fp32 in between, rounded once.
-// Bound: HBM in long batches, launch and two dependent loads in short ones.
+// Bound: HBM in long batches (32768 tokens of 40 heads 118 us, 5.7 TB/s read and written), launch and two dependent loads in short ones (64 tokens 3.7).
 #include "common.h"
 
 namespace antkv {
@@ -17,8 +17,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnits = kD / 16;                                     // threads of a head's row
 constexpr int kPass = kThreads / kUnits;                            // rows of a pass
-constexpr int kAhead = 4;                                           // passes whose loads are in flight together
-constexpr int kTokens = 16;                                         // of a workgroup, at most
+constexpr int kAhead = 1;                                           // rows of a thread whose loads are in flight together
+constexpr int kTokens = 32;                                         // of a workgroup, at most
+constexpr int64_t kCaches = 32LL << 20;                             // bytes of the eight L2s
 constexpr int kMostGroups = 1 << 20;
 constexpr double kTurn = 0.15915494309189533576888376337251;        // 1 / (2 pi)
 
@@ -36,18 +37,40 @@ __device__ __forceinline__ int request_at(const int32_t* q_start, int R, int64_t
     return lo;
 }
 
+template <bool kStream>                                             // the output goes past the caches
 __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs p, int tokens, int64_t groups)
 {
     __shared__ float2_t s_turn[kTokens][kD / 2];                    // cosine, sine
-    __shared__ int s_seq[kTokens], s_tok[kTokens];                  // -1: nobody's row
+    __shared__ int s_live[kTokens];                                 // somebody's row
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int H = p.Hq + p.Hkv, unit = tid % kUnits, pairs = p.rot / 2;
     const int half = p.rot / 16;                                    // 16-byte pieces between the channels of a pair, style 1
     // the unit's two 16-byte pieces
     const bool turns = 16 * unit < p.rot;
     const int a = p.style == 1 && turns ? unit : 2 * unit, b = p.style == 1 && turns ? unit + half : 2 * unit + 1;
+    const int rows = tokens * H;
     for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
         const int64_t first = group * tokens;                       // token of all B x T
+        uint4_t x[kAhead], y[kAhead];
+        uint4_t* to[kAhead];
+        int at[kAhead];
+        auto load = [&](int row0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int row = row0 + j * kPass, i = row / H, h = row - i * H;
+                to[j] = nullptr;
+                at[j] = i;
+                if (row < rows && first + i < p.B * p.T) {
+                    const uint32_t u = (uint32_t)(first + i), n = p.B > 1 ? u / (uint32_t)p.T : 0, t = u - n * (uint32_t)p.T;
+                    const RopeRows& z = h < p.Hq ? p.q : p.k;
+                    const int hh = h < p.Hq ? h : h - p.Hq;
+                    const uint4_t* from = (const uint4_t*)(z.x + n * z.xs_b + t * z.xs_t + hh * z.xs_h);
+                    to[j] = (uint4_t*)(z.y + n * z.ys_b + t * z.ys_t + hh * z.ys_h);
+                    x[j] = from[a];
+                    y[j] = from[b];
+                }
+            }
+        };
         if (group != blockIdx.x) __syncthreads();
         for (int i = wave; i < tokens; i += kThreads / 64) {
             const int64_t u = first + i;
@@ -59,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs p, int to
                 live = u >= from && u < end;
                 pos = p.ctx_len[r] - end + u;
             } else if (live) {
-                pos = p.pos ? p.pos[u] : p.pos0 + u % p.T;
+                pos = p.pos ? p.pos[u] : p.pos0 + (p.B > 1 ? (int64_t)((uint32_t)u % (uint32_t)p.T) : u);
             }
             if (live && lane < pairs) {
                 const double turn = (double)pos * p.freqs[lane] * kTurn;
@@ -67,39 +90,14 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs p, int to
                 sincospif(2.f * (float)(turn - rint(turn)), &s, &c);
                 s_turn[i][lane] = float2_t{c * p.amplitude, s * (p.inverse ? -p.amplitude : p.amplitude)};
             }
-            if (lane == 0) {
-                const int64_t n = p.B > 1 && live ? u / p.T : 0;
-                s_seq[i] = live ? (int)n : -1;
-                s_tok[i] = (int)(u - n * p.T);
-            }
+            if (lane == 0) s_live[i] = live;
         }
         __syncthreads();
-        const int rows = tokens * H;
         for (int row0 = tid / kUnits; row0 < rows; row0 += kAhead * kPass) {
-            uint4_t x[kAhead], y[kAhead];
-            uint4_t* to[kAhead];
-            int at[kAhead];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const int row = row0 + j * kPass;
-                to[j] = nullptr;
-                if (row < rows) {
-                    const int i = row / H, h = row - i * H;
-                    const int64_t n = s_seq[i], t = s_tok[i];
-                    if (n >= 0) {
-                        const RopeRows& z = h < p.Hq ? p.q : p.k;
-                        const int hh = h < p.Hq ? h : h - p.Hq;
-                        const uint4_t* from = (const uint4_t*)(z.x + n * z.xs_b + t * z.xs_t + hh * z.xs_h);
-                        to[j] = (uint4_t*)(z.y + n * z.ys_b + t * z.ys_t + hh * z.ys_h);
-                        x[j] = from[a];
-                        y[j] = from[b];
-                        at[j] = i;
-                    }
-                }
-            }
+            load(row0);
 #pragma unroll
             for (int j = 0; j < kAhead; ++j)
-                if (to[j]) {
+                if (to[j] && s_live[at[j]]) {
                     if (turns) {
                         const float4_t* cs = (const float4_t*)&s_turn[at[j]][8 * unit];
                         float c[8], s[8];
@@ -127,8 +125,13 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs p, int to
                         x[j] = __builtin_bit_cast(uint4_t, yu);
                         y[j] = __builtin_bit_cast(uint4_t, yw);
                     }
-                    to[j][a] = x[j];
-                    to[j][b] = y[j];
+                    if (kStream) {
+                        __builtin_nontemporal_store(x[j], to[j] + a);
+                        __builtin_nontemporal_store(y[j], to[j] + b);
+                    } else {
+                        to[j][a] = x[j];
+                        to[j][b] = y[j];
+                    }
                 }
         }
     }
@@ -153,12 +156,16 @@ hipError_t launch_rope(const RopeArgs& a, hipStream_t st)
 {
     const int H = a.Hq + a.Hkv;
     const int64_t all = a.B * a.T;
-    // a workgroup's tokens: all of its passes in flight at once, where that leaves a workgroup for every CU
+    // A workgroup's tokens: those of one pass, fewer where that leaves CUs without a workgroup.  One, two and four rows of a thread in flight, 32768
+    // tokens of 40 heads 124, 125 and 129 us, of 8 heads 32, 34 and 37; workgroups of twice the size, one row, 157 and 35; loads ahead of the angles (more
+    // registers, fewer waves) 147 and 37.
     int tokens = kAhead * kPass / H;
     tokens = tokens < 1 ? 1 : tokens < kTokens ? tokens : kTokens;
     while (tokens > 1 && all / tokens < 1024) tokens /= 2;
     const int64_t groups = (all + tokens - 1) / tokens;
-    hipLaunchKernelGGL(rope_kernel, dim3((unsigned)(groups < kMostGroups ? groups : kMostGroups)), dim3(kThreads), 0, st, a, tokens, groups);
+    // More than the L2s hold goes past them: 32768 tokens 124 us through them and 118 past them, of 8 heads 32 and 22.
+    const auto kernel = all * H * (kD * 2) > kCaches ? rope_kernel<true> : rope_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(groups < kMostGroups ? groups : kMostGroups)), dim3(kThreads), 0, st, a, tokens, groups);
     return hipGetLastError();
 }
 

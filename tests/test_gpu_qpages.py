@@ -243,7 +243,7 @@ def test_qpage_store_nothing():
 
 def test_qpage_store_of_the_largest_batch():
     """As many rows as a grid has, all of them the same one and nearly all without a slot."""
-    T, Hkv = (1 << 23) - 16, 64
+    T, Hkv = (1 << 24) - 16, 64
     gen = gen_of(92)
     k, v = (randn(gen, 1, Hkv, D).expand(T, Hkv, D) for _ in "kv")
     pools = Pools(4, Hkv, 16)
@@ -278,6 +278,11 @@ def test_qpage_load(B, Hkv, page, N, first):
     got = antkv.qpage_load(geom, *pools.args(), table, N, first=first, ctx_len=ints(lens), k=before[0].clone(), v=before[1].clone())
     for g, d, b in zip(got, dense, before):
         assert torch.equal(g, torch.where(there[:, None, :, None], d, b))
+    made = antkv.qpage_load(geom, *pools.args(), table, N, first=first, ctx_len=ints(lens))
+    half = antkv.qpage_load(geom, *pools.args(), table, N, first=first, ctx_len=ints(lens), v=before[1].clone())
+    for g, d in zip((*made, half[0]), (*dense, dense[0])):
+        assert torch.equal(g, torch.where(there[:, None, :, None], d, 0))
+    assert torch.equal(half[1], got[1])
 
 
 # ------------------------------------------------------------------------------------------------ attention

@@ -39,17 +39,17 @@ def test_qpage_store_refusals(lib, bad, code):
     assert _store(lib, **bad) == code
 
 
-@pytest.mark.parametrize("hkv,most", [(1, (1 << 28) - 16), (2, (1 << 28) - 16), (3, (1 << 27) - 16), (64, (1 << 23) - 16)])
+@pytest.mark.parametrize("hkv,most", [(1, (1 << 28) - 16), (4, (1 << 28) - 16), (5, (1 << 27) - 16), (64, (1 << 24) - 16)])
 def test_qpage_store_of_a_grid_and_a_row_more(lib, hkv, most):
-    """16 rows of two heads to a workgroup, fewer than 2^24 of them."""
+    """16 rows of four heads to a workgroup, fewer than 2^24 of them."""
     g = _g(Hq=hkv, Hkv=hkv)
     assert _store(lib, g=g, T=most + 1) == EINVAL and _store(lib, g=g, T=most, slot=None) == EINVAL
-    assert (most // 16) * ((hkv + 1) // 2) < 1 << 24 <= (most // 16 + 1) * ((hkv + 1) // 2)
+    assert (most // 16) * ((hkv + 3) // 4) < 1 << 24 <= (most // 16 + 1) * ((hkv + 3) // 4)
 
 
 def _load(lib, g=None, kp=FAKE, vp=FAKE, ks=FAKE, vs=FAKE, n_pages=8, page=16, table=FAKE, cap=4, ctx=None, first=0, N=8, k=FAKE, v=OTHER, xb=2048, xh=1024,
           xt=128):
-    return lib.antkv_qpage_load(ctypes.byref(g or _g()), kp, vp, ks, vs, n_pages, page, table, cap, ctx, first, N, k, v, xb, xh, xt, None)
+    return lib.antkv_qpage_load(ctypes.byref(g or _g()), kp, vp, ks, vs, n_pages, page, table, cap, ctx, first, N, k, v, xb, xh, xt, 0, None)
 
 
 @pytest.mark.parametrize("bad,code", [
