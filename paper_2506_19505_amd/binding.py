@@ -612,18 +612,36 @@ def page_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Tens
 
 # ---- the same cache in 8 bits -------------------------------------------------------------------------------------------
 
+# Host cost of a call: with every check a function call of its own, 4.5 of the 11.3 us of qpage_attn.  Below each call asks in one go whether
+# all is well, and only otherwise what is wrong.
+
+_E4M3, _HALF, _FLOAT, _INT = torch.float8_e4m3fn, torch.float16, torch.float32, torch.int32
+
+
 def _byte_pools(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, heads: int):
-    _need(k_pages, torch.float8_e4m3fn, "k_pages")
-    _need(v_pages, torch.float8_e4m3fn, "v_pages")
-    _need(k_scales, torch.float32, "k_scales")
-    _need(v_scales, torch.float32, "v_scales")
-    shape = k_pages.shape
+    """-> n_pages, page_size, device"""
+    shape, device = k_pages.shape, k_pages.get_device()
+    if (k_pages.dtype is _E4M3 and v_pages.dtype is _E4M3 and k_scales.dtype is _FLOAT and v_scales.dtype is _FLOAT and len(shape) == 4
+            and v_pages.shape == shape and device >= 0 and device == v_pages.get_device() == k_scales.get_device() == v_scales.get_device()):
+        n_pages, h, page_size, d = shape
+        if (h == heads and d == 128 and k_scales.shape == (n_pages, heads, page_size // 16) and v_scales.shape == k_scales.shape
+                and k_pages.is_contiguous() and v_pages.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
+            return n_pages, page_size, device
+    _need(k_pages, _E4M3, "k_pages")
+    _need(v_pages, _E4M3, "v_pages")
+    _need(k_scales, _FLOAT, "k_scales")
+    _need(v_scales, _FLOAT, "v_scales")
     if len(shape) != 4 or shape[1] != heads or shape[3] != 128 or v_pages.shape != shape:
         raise ValueError(f"k_pages and v_pages must be [n_pages, {heads}, page_size, 128]")
-    n_pages, page_size = shape[0], shape[2]
-    if k_scales.shape != (n_pages, heads, page_size // 16) or v_scales.shape != k_scales.shape:
-        raise ValueError(f"k_scales and v_scales must be [{n_pages}, {heads}, {page_size // 16}]")
-    return n_pages, page_size
+    if k_scales.shape != (shape[0], heads, shape[2] // 16) or v_scales.shape != k_scales.shape:
+        raise ValueError(f"k_scales and v_scales must be [{shape[0]}, {heads}, {shape[2] // 16}]")
+    raise ValueError("all tensors must be on the same device")
+
+
+def _on(device: int, *tensors):
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("all tensors must be on the same device" if t.is_cuda else "all tensors must be device tensors")
 
 
 def qpage_store(geom: Geometry, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor,
@@ -632,15 +650,17 @@ def qpage_store(geom: Geometry, k: torch.Tensor, v: torch.Tensor, slot: torch.Te
     float8_e4m3fn [n_pages,Hkv,page_size,D] with scales fp32 [n_pages,Hkv,page_size/16]."""
     heads = geom.Hkv
     _rows(k, "k", heads)
-    n_pages, page_size = _byte_pools(k_pages, v_pages, k_scales, v_scales, heads)
-    T = k.shape[0]
-    if v.shape != k.shape or v.stride() != k.stride() or v.dtype is not torch.float16:
+    n_pages, page_size, device = _byte_pools(k_pages, v_pages, k_scales, v_scales, heads)
+    T, strides = k.shape[0], k.stride()
+    if v.shape != k.shape or v.stride() != strides or v.dtype is not _HALF:
         _rows(v, "v", heads)
-        if v.shape[0] != T or (T > 1 and v.stride(0) != k.stride(0)) or (heads > 1 and v.stride(1) != k.stride(1)):
+        if v.shape[0] != T or (T > 1 and v.stride(0) != strides[0]) or (heads > 1 and v.stride(1) != strides[1]):
             raise ValueError("k and v must have the same shape and strides")
-    _ints(slot, "slot", (T,))
-    _run(load_library().antkv_qpage_store, "antkv_qpage_store", _one_device(k_pages, v_pages, k_scales, v_scales, k, v, slot), geom._c, k.data_ptr(),
-         v.data_ptr(), k.stride(0) if T > 1 else 0, k.stride(1) if heads > 1 else 0, T, slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+    if slot.dtype is not _INT or slot.shape != (T,) or not slot.is_contiguous():
+        _ints(slot, "slot", (T,))
+    _on(device, k, v, slot)
+    _run(load_library().antkv_qpage_store, "antkv_qpage_store", device, geom._c, k.data_ptr(),
+         v.data_ptr(), strides[0] if T > 1 else 0, strides[1] if heads > 1 else 0, T, slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
          k_scales.data_ptr(), v_scales.data_ptr(), n_pages, page_size, _stream(k_pages))
 
 
@@ -648,7 +668,7 @@ def qpage_load(geom: Geometry, k_pages: torch.Tensor, v_pages: torch.Tensor, k_s
                first: int = 0, ctx_len: torch.Tensor | None = None, k: torch.Tensor | None = None, v: torch.Tensor | None = None):
     """antkv_qpage_load: positions first .. first + N - 1 of the table's requests -> (k, v) fp16 [B,Hkv,N,D].  Rows at or behind
     ctx_len (int32 [B]) are left as they are: zeros where k and v are made here."""
-    n_pages, page_size = _byte_pools(k_pages, v_pages, k_scales, v_scales, geom.Hkv)
+    n_pages, page_size, device = _byte_pools(k_pages, v_pages, k_scales, v_scales, geom.Hkv)
     cap = _table(table, geom.B)
     if ctx_len is not None:
         _ints(ctx_len, "ctx_len", (geom.B,))
@@ -665,8 +685,9 @@ def qpage_load(geom: Geometry, k_pages: torch.Tensor, v_pages: torch.Tensor, k_s
         _need(v, torch.float16, "v")
         if k.shape != shape or v.shape != shape:
             raise ValueError(f"k and v must be {list(shape)}")
+    _on(device, table, ctx_len, k, v)
     rows = N * geom.D
-    _run(load_library().antkv_qpage_load, "antkv_qpage_load", _one_device(k_pages, v_pages, k_scales, v_scales, table, ctx_len, k, v), geom._c,
+    _run(load_library().antkv_qpage_load, "antkv_qpage_load", device, geom._c,
          k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n_pages, page_size, table.data_ptr(), cap, _p(ctx_len), first, N,
          k.data_ptr(), v.data_ptr(), geom.Hkv * rows, rows, geom.D, clear, _stream(k_pages))
     return k, v
@@ -687,15 +708,17 @@ def qpage_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Ten
     """antkv_qpage_attn: page_attn over pools float8_e4m3fn [n_pages,Hkv,page_size,D] with scales fp32 [n_pages,Hkv,page_size/16]."""
     Hq, R = geom.Hq, geom.B
     _rows(q, "q", Hq)
-    n_pages, page_size = _byte_pools(k_pages, v_pages, k_scales, v_scales, geom.Hkv)
-    T = q.shape[0]
-    _ints(q_start, "q_start", (R + 1,))
-    _ints(ctx_len, "ctx_len", (R,))
-    cap = _table(table, R)
+    n_pages, page_size, device = _byte_pools(k_pages, v_pages, k_scales, v_scales, geom.Hkv)
+    T, strides, held = q.shape[0], q.stride(), table.shape
+    if (q_start.dtype is not _INT or ctx_len.dtype is not _INT or table.dtype is not _INT or q_start.shape != (R + 1,) or ctx_len.shape != (R,) or len(held) != 2
+            or held[0] != R or not (q_start.is_contiguous() and ctx_len.is_contiguous() and table.is_contiguous())):
+        _ints(q_start, "q_start", (R + 1,))
+        _ints(ctx_len, "ctx_len", (R,))
+        _table(table, R)
     if out is None:
         out = q.new_empty((T, Hq, 128))
     else:
-        _need(out, torch.float16, "out")
+        _need(out, _HALF, "out")
         if out.shape != q.shape:
             raise ValueError("out must have the shape of q")
     row_max = row_sum = None
@@ -705,8 +728,9 @@ def qpage_attn(geom: Geometry, q: torch.Tensor, scale: float, q_start: torch.Ten
         workspace = _workspace(load_library().antkv_qpage_attn_workspace(geom._c, T), q.device)
     else:
         _need(workspace, torch.uint8, "workspace")
-    _run(load_library().antkv_qpage_attn, "antkv_qpage_attn", _one_device(q, k_pages, v_pages, k_scales, v_scales, q_start, ctx_len, table, out, workspace),
-         geom._c, q.data_ptr(), q.stride(0) if T > 1 else 0, q.stride(1) if Hq > 1 else 0, T, q_start.data_ptr(), ctx_len.data_ptr(), table.data_ptr(), cap,
+    _on(device, q, q_start, ctx_len, table, out, workspace)
+    _run(load_library().antkv_qpage_attn, "antkv_qpage_attn", device, geom._c, q.data_ptr(), strides[0] if T > 1 else 0,
+         strides[1] if Hq > 1 else 0, T, q_start.data_ptr(), ctx_len.data_ptr(), table.data_ptr(), held[1],
          k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n_pages, page_size, float(scale), int(window), int(n_sink),
          out.data_ptr(), _p(row_max), _p(row_sum), workspace.data_ptr(), workspace.numel(), _stream(q))
     return out, row_max, row_sum
@@ -728,7 +752,7 @@ def rope_freqs(rot_dim: int = 128, base: float = 10000.0, factor: float = 1.0, t
 
 def _rope_rows(x: torch.Tensor, out: torch.Tensor | None, name: str, heads: int, batch: int, packed: bool):
     """x fp16 [T,heads,D] (packed, or one sequence) or [B,heads,T,D], channels contiguous -> (T, out, strides b, t, h of x, of out)."""
-    shape = x.shape
+    shape, a = x.shape, x.stride()
     if len(shape) == 3:
         T, h, d = shape
         fits = packed or batch == 1
@@ -739,9 +763,8 @@ def _rope_rows(x: torch.Tensor, out: torch.Tensor | None, name: str, heads: int,
         fits = False
     if not x.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if x.dtype is not torch.float16:
+    if x.dtype is not _HALF:
         raise TypeError(f"{name} must be torch.float16")
-    a = x.stride()
     if not fits or h != heads or d != 128 or a[-1] != 1:
         raise ValueError(f"{name} must be [T, {heads}, 128] of a packed batch or of one sequence, or [{batch}, {heads}, T, 128], with contiguous channels")
     if out is None:
@@ -767,8 +790,9 @@ def rope(geom: Geometry, q: torch.Tensor | None, k: torch.Tensor | None, freqs: 
     (q_out, k_out), made here where they are not given; q_out=q turns q in place.  Rows outside a packed batch's requests are left as they
     are (undefined where the output is made here)."""
     packed = q_start is not None
-    _need(freqs, torch.float64, "freqs")
-    if freqs.dim() != 1:
+    rot = freqs.shape
+    if freqs.dtype is not torch.float64 or len(rot) != 1 or not freqs.is_contiguous():
+        _need(freqs, torch.float64, "freqs")
         raise ValueError("freqs must be [rot_dim / 2]")
     first = k if q is None else q
     if first is None:
@@ -779,12 +803,17 @@ def rope(geom: Geometry, q: torch.Tensor | None, k: torch.Tensor | None, freqs: 
     if q is not None and k is not None and (Tq != Tk or q.dim() != k.dim()):
         raise ValueError("q and k must have the same rows")
     if packed:
-        _ints(q_start, "q_start", (geom.B + 1,))
+        R = geom.B
         if ctx_len is None:
             raise ValueError("q_start needs ctx_len")
-        _ints(ctx_len, "ctx_len", (geom.B,))
+        if (q_start.dtype is not _INT or ctx_len.dtype is not _INT or q_start.shape != (R + 1,) or ctx_len.shape != (R,)
+                or not (q_start.is_contiguous() and ctx_len.is_contiguous())):
+            _ints(q_start, "q_start", (R + 1,))
+            _ints(ctx_len, "ctx_len", (R,))
     if pos is not None:
         _ints(pos, "pos", (T,) if first.dim() == 3 else (geom.B, T))
-    _run(load_library().antkv_rope, "antkv_rope", _one_device(first, q, k, freqs, pos, q_start, ctx_len), geom._c, *qs[:4], *ks[:4], T, _p(pos), _p(q_start),
-         _p(ctx_len), pos0, freqs.data_ptr(), 2 * freqs.shape[0], style, amplitude, inverse, *qs[4:], *ks[4:], _stream(first))
+    device = first.get_device()
+    _on(device, q, k, freqs, pos, q_start, ctx_len)
+    _run(load_library().antkv_rope, "antkv_rope", device, geom._c, *qs[:4], *ks[:4], T, _p(pos), _p(q_start), _p(ctx_len), pos0, freqs.data_ptr(), 2 * rot[0],
+         style, amplitude, inverse, *qs[4:], *ks[4:], _stream(first))
     return q_out, k_out

@@ -15,6 +15,7 @@ namespace {
 using namespace paged;
 
 struct Fp16Pages {
+    static constexpr int kTileNarrow = 1, kTileWide = 1;            // the unit of cost
     // What a block costs beside its key tiles.  Narrow 14, 20, 28: 16 tokens on 300 keys each 11.0, 15.0, 16.2 us, 63 tokens beside one chunk of 100 on 2000
     // keys each 105, 106, 118, 64 on 1 .. 32768 keys 147, 148, 147 (4, measured earlier: 208 where 20 took 176).  Wide 12, 16, 20: 300 tokens on 2000
     // keys 46, 38, 46, 8 prompts of 1024 131, 121, 119
@@ -22,6 +23,7 @@ struct Fp16Pages {
     // The smallest shares.  8, 12, 16: a token on 4096 keys 14.7, 13.2, 13.8 us, one each of 4 requests on 2048 keys 16.6, 14.5, 14.9; 16, 24, 32: 64
     // tokens on 4096 keys 32.5, 33.9, 36.0, 300 on 2000 39.4, 38.1, 46.2, 4 x 100 on 1000 32.1, 31.4, 32.0
     static constexpr int kLeastNarrow = 12, kLeastWide = 24;
+    static constexpr int kFirst = 4;                                // key tiles of a block's first piece, at least
     static constexpr int kRowsOfEight = 1024;                       // of a request on average, and a KV head: for workgroups of eight waves
 
     template <int NW>                                       // waves of a workgroup: 8 or 4

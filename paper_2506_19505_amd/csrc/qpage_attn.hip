@@ -61,13 +61,16 @@ struct ByteOperands {
 };
 
 struct BytePages {
-    // As page_attn.hip's, measured again.  What a narrow block costs beside its tiles, 14, 16, 20: 64 tokens on 1 .. 32768 keys each 88.0, 85.2, 84.1 us, 128 on
-    // 1 .. 16384 113, 105, 111, 300 x 20 on 40 .. 1500 150, 144, 161, 16 on 300 each 11.6, 12.7, 13.2.  A wide one, 16 and 24: 300 tokens on 2000 keys 42 and 49, 8
-    // prompts of 1024 131 and 126, 64 tokens on 4096 38 and 42
-    static constexpr int kIdleNarrow = 16, kIdleWide = 16;
-    // The smallest shares.  12 and 18: a token on 4096 keys 12.5 and 13.5 us, one each of 4 requests on 2048 13.7 and 14.5; 24 and 36: 300 tokens on 2000 keys 42
-    // and 52
-    static constexpr int kLeastNarrow = 12, kLeastWide = 24;
+    // Costs of key tiles, in quarters of a wide block's: four waves share a narrow block's, a workgroup each works on 0.25 and 1.0 us a tile side by side (a
+    // narrow one 0.5 where all are).  As one and as half: 16 requests with 2048 tokens among them 87 and 81 us, 300 x 20 on 40 .. 1500 144 and 126, 64
+    // tokens on 1 .. 32768 keys each 87 and 85.
+    static constexpr int kTileNarrow = 2, kTileWide = 4;
+    // Of coming and going: 10 and 15 us a block (pages, scales, first tiles 5, partial sums 4).  Narrow, 32 and 40: 64 tokens on 1 .. 32768 keys 88 and 85 us
+    static constexpr int kIdleNarrow = 40, kIdleWide = 64;
+    // The smallest shares.  24 and 36: a token on 4096 keys 12.5 and 13.5 us; 96 and 144: 300 tokens on 2000 keys 42 and 52
+    static constexpr int kLeastNarrow = 24, kLeastWide = 96;
+    // Key tiles of a block's first piece, at least.  4 and 8: 16 tokens on 300 keys each 13.6 and 12.7 us, 4 x 100 on 1000 36.3 and 34.9
+    static constexpr int kFirst = 8;
     // 1024 and 512: 16 requests with 2048 tokens among them 88 and 102 us; 1024 and 256: 64 tokens on 4096 keys 39 and 50
     static constexpr int kRowsOfEight = 1024;
 
