@@ -52,13 +52,13 @@ struct Cost {
         a = step = 0;
         if (blocks > 0) {
             const int first = (blocks - 1) * (kRows >> p.gs);
-            a = span_of(q.p0 + first, q.p0 + q.n - 1, q.limit, p.window, p.n_sink).n * tile(rows) + idle(rows);
+            a = (span_of(q.p0 + first, q.p0 + q.n - 1, q.limit, p.window, p.n_sink).n << shift(rows)) + idle(rows);
             // causal: each block sees as many tiles less as it has tokens / 32; not so in a window, or where the table ends early
-            if (p.window == 0 && q.p0 >= 0 && q.p0 + q.n <= q.limit) step = (kRows / 32 >> p.gs) * tile(rows);
+            if (p.window == 0 && q.p0 >= 0 && q.p0 + q.n <= q.limit) step = kRows / 32 >> p.gs << shift(rows);
         }
     }
-    // of a key tile; of coming and going: looking up pages, the first loads, partial sums
-    __device__ __forceinline__ static int tile(int rows) { return rows <= kNarrow ? Cache::kTileNarrow : Cache::kTileWide; }
+    // of a key tile, as a power of two; of coming and going: looking up pages, the first loads, partial sums
+    __device__ __forceinline__ static int shift(int rows) { return rows <= kNarrow ? Cache::kShiftNarrow : Cache::kShiftWide; }
     __device__ __forceinline__ static int idle(int rows) { return rows <= kNarrow ? Cache::kIdleNarrow : Cache::kIdleWide; }
     __device__ __forceinline__ int before(int k) const { return k * a - step * (k * (k - 1) / 2); }      // of blocks 0 .. k - 1
     __device__ __forceinline__ int all() const { return before(blocks); }
@@ -328,11 +328,11 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
         bool some = true;                                           // the piece has tiles, or is the only one
         if (!p.unit) {
             // cost offset -> tile: what lies behind the idle part, cut at every fourth (wide blocks are worked on four at a time)
-            const int idle = Cost<Cache, NW>::idle(rows), each = Cost<Cache, NW>::tile(rows), round = 4;
-            auto tile_at = [&](int off) { const int t = (off - idle) / each; return t <= 0 ? 0 : off >= len ? span.n : t / round * round < span.n ? t / round * round : span.n; };
+            const int idle = Cost<Cache, NW>::idle(rows), shift = Cost<Cache, NW>::shift(rows), round = 4;
+            auto tile_at = [&](int off) { const int t = (off - idle) >> shift; return t <= 0 ? 0 : off >= len ? span.n : t / round * round < span.n ? t / round * round : span.n; };
             all.start = c0 >= share * size ? share : c0 / size;
             all.last = c0 + len <= (share + 1) * size ? share : (c0 + len - 1) / size;
-            all.first = (c0 + idle + Cache::kFirst * each + size - 1) / size - 1;       // the first with so many tiles
+            all.first = (c0 + idle + (Cache::kFirst << shift) + size - 1) / size - 1;   // the first with so many tiles
             if (all.first < all.start) all.first = all.start;
             if (all.first > all.last) all.first = all.last;
             some = share >= all.first;
@@ -447,7 +447,7 @@ inline int rows_cap_of(const Geom& g, int64_t T, int nw) { return T * g.G < 32 *
 template <class Cache>
 inline bool unit_blocks(const Geom& g, int64_t T, int64_t most, int64_t longest)
 {
-    return (T >= 2048 * (int64_t)g.B && T * g.G / 256 * g.Hkv >= 2 * kWaves / 8) || most > (1LL << 30) / ((longest / 32 + 32) * Cache::kTileWide);
+    return (T >= 2048 * (int64_t)g.B && T * g.G / 256 * g.Hkv >= 2 * kWaves / 8) || most > (1LL << 30) / ((longest / 32 + 32) << Cache::kShiftWide);
 }
 
 // What either would need: a workspace made for many tokens then does for fewer.

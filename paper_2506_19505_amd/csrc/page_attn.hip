@@ -15,7 +15,7 @@ namespace {
 using namespace paged;
 
 struct Fp16Pages {
-    static constexpr int kTileNarrow = 1, kTileWide = 1;            // the unit of cost
+    static constexpr int kShiftNarrow = 0, kShiftWide = 0;          // a key tile costs 1
     // What a block costs beside its key tiles.  Narrow 14, 20, 28: 16 tokens on 300 keys each 11.0, 15.0, 16.2 us, 63 tokens beside one chunk of 100 on 2000
     // keys each 105, 106, 118, 64 on 1 .. 32768 keys 147, 148, 147 (4, measured earlier: 208 where 20 took 176).  Wide 12, 16, 20: 300 tokens on 2000
     // keys 46, 38, 46, 8 prompts of 1024 131, 121, 119

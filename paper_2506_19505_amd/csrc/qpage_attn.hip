@@ -61,10 +61,10 @@ struct ByteOperands {
 };
 
 struct BytePages {
-    // Costs of key tiles, in quarters of a wide block's: four waves share a narrow block's, a workgroup each works on 0.25 and 1.0 us a tile side by side (a
+    // Costs of key tiles, 2 and 4: four waves share a narrow block's, a workgroup each works on 0.25 and 1.0 us a tile side by side (a
     // narrow one 0.5 where all are).  As one and as half: 16 requests with 2048 tokens among them 87 and 81 us, 300 x 20 on 40 .. 1500 144 and 126, 64
     // tokens on 1 .. 32768 keys each 87 and 85.
-    static constexpr int kTileNarrow = 2, kTileWide = 4;
+    static constexpr int kShiftNarrow = 1, kShiftWide = 2;
     // Of coming and going: 10 and 15 us a block (pages, scales, first tiles 5, partial sums 4).  Narrow, 32 and 40: 64 tokens on 1 .. 32768 keys 88 and 85 us
     static constexpr int kIdleNarrow = 40, kIdleWide = 64;
     // The smallest shares.  24 and 36: a token on 4096 keys 12.5 and 13.5 us; 96 and 144: 300 tokens on 2000 keys 42 and 52
@@ -414,6 +414,9 @@ struct BytePages {
                 });
                 end(i, T);
             };
+            // Two workgroups of a CU: the one that came first would have the matrix units first as well, and be done long before the other (16 requests with
+            // 2048 tokens among them 83 us, 300 x 20 tokens on 40 .. 1500 keys 127; 78 and 119 this way round)
+            if (NW == 4 && (blockIdx.x >> 8 & 1)) __builtin_amdgcn_s_setprio(1);
             if (active) {
 #pragma unroll 1
                 for (int i = 0; i < m; i += 4) {
@@ -433,6 +436,7 @@ struct BytePages {
                     end(i, i);
                 }
             }
+            if (NW == 4) __builtin_amdgcn_s_setprio(0);
             wait_all_loads();                                       // nothing may land in LDS after the turn, or the workgroup's end
         }
         sums.join_halves();
