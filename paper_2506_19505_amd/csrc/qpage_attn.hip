@@ -257,9 +257,10 @@ struct BytePages {
         const int row = w_row + n < rows ? w_row + n : rows - 1;
         const Sight sight(p, rq.p0 + (row >> p.gs), rq.limit);
 
-        // staging: lane's row of the piece's eight, so that the 16 lanes that write together have rows four apart (banks); rows behind the last key
-        // that the workgroup sees repeat it
-        const int part = wave & 3, half = part >> 1, r = 8 * part + (lane >> 4) + 4 * (lane >> 3 & 1), chunk = lane & 7;
+        // staging: lane's row of the piece's eight and 16 bytes of it.  Eight lanes have four pieces each of two rows four apart: what they write
+        // together, every other 16 bytes of the halves, then falls on different banks (of 128 bytes at a time).  Rows behind the last key that the
+        // workgroup sees repeat it
+        const int part = wave & 3, half = part >> 1, r = 8 * part + (lane >> 4) + 4 * (lane >> 2 & 1), chunk = (lane & 3) + 4 * (lane >> 3 & 1);
         const int last_tile = (span.keys - 1) >> 5, last_key = (span.keys - 1) & 31;
         const uint32_t soff = (r & 15) * kD + chunk * 16, soff_last = ((r < last_key ? r : last_key) & 15) * kD + chunk * 16;
         const uint32_t bytes0 = lds0 + 4 * kTileBytes + part * 1024;                       // of K in slot 0; V 4 tiles on
