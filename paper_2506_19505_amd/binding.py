@@ -750,29 +750,31 @@ def rope_freqs(rot_dim: int = 128, base: float = 10000.0, factor: float = 1.0, t
     return freqs
 
 
-def _rope_rows(x: torch.Tensor, out: torch.Tensor | None, name: str, heads: int, batch: int, packed: bool):
-    """x fp16 [T,heads,D] (packed, or one sequence) or [B,heads,T,D], channels contiguous -> (T, out, strides b, t, h of x, of out)."""
+def _rope_rows(x: torch.Tensor, out: torch.Tensor | None, name: str, heads: int, batch: int, packed: bool, device: int):
+    """x fp16 [T,heads,D] (packed, or one sequence) or [B,heads,T,D], channels contiguous -> (T, out, address and strides b, t, h of x, of out)."""
     shape, a = x.shape, x.stride()
-    if len(shape) == 3:
+    if len(a) == 3:
         T, h, d = shape
         fits = packed or batch == 1
-    elif len(shape) == 4:
+    elif len(a) == 4:
         b, h, T, d = shape
         fits = b == batch and not packed
     else:
         fits = False
-    if not x.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if x.dtype is not _HALF:
-        raise TypeError(f"{name} must be torch.float16")
-    if not fits or h != heads or d != 128 or a[-1] != 1:
+    if not fits or h != heads or d != 128 or a[-1] != 1 or x.dtype is not _HALF or x.get_device() != device or device < 0:
+        if not x.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        if x.dtype is not _HALF:
+            raise TypeError(f"{name} must be torch.float16")
+        if x.get_device() != device:
+            raise ValueError("all tensors must be on the same device")
         raise ValueError(f"{name} must be [T, {heads}, 128] of a packed batch or of one sequence, or [{batch}, {heads}, T, 128], with contiguous channels")
     if out is None:
         out = x.new_empty(shape)
-        o = out.stride()
+        o = (128 * h, 128) if len(a) == 3 else (128 * T * h, 128 * T, 128)
     else:
         o = out.stride()
-        if out is not x and (out.get_device() != x.get_device() or out.dtype is not torch.float16 or out.shape != shape or o[-1] != 1):
+        if out is not x and (out.get_device() != device or out.dtype is not _HALF or out.shape != shape or o[-1] != 1):
             raise ValueError(f"{name}_out must be like {name}")
     if len(a) == 3:
         return T, out, x.data_ptr(), 0, a[0], a[1], out.data_ptr(), 0, o[0], o[1]
@@ -789,31 +791,30 @@ def rope(geom: Geometry, q: torch.Tensor | None, k: torch.Tensor | None, freqs: 
     sequence, or [B,Hq,T,D] and [B,Hkv,T,D]; positions pos (int32, [T] or [B,T]) or pos0, pos0 + 1, ..; freqs fp64 [rot_dim/2] (rope_freqs) ->
     (q_out, k_out), made here where they are not given; q_out=q turns q in place.  Rows outside a packed batch's requests are left as they
     are (undefined where the output is made here)."""
-    packed = q_start is not None
+    first = k if q is None else q
+    if first is None:
+        raise ValueError("q or k must be given")
+    packed, device, B = q_start is not None, first.get_device(), geom.B
     rot = freqs.shape
     if freqs.dtype is not torch.float64 or len(rot) != 1 or not freqs.is_contiguous():
         _need(freqs, torch.float64, "freqs")
         raise ValueError("freqs must be [rot_dim / 2]")
-    first = k if q is None else q
-    if first is None:
-        raise ValueError("q or k must be given")
-    Tq, q_out, *qs = _NO_ROWS if q is None else _rope_rows(q, q_out, "q", geom.Hq, geom.B, packed)
-    Tk, k_out, *ks = _NO_ROWS if k is None else _rope_rows(k, k_out, "k", geom.Hkv, geom.B, packed)
-    T = Tk if q is None else Tq
-    if q is not None and k is not None and (Tq != Tk or q.dim() != k.dim()):
+    T, q_out, q0, qb, qt, qh, qo0, qob, qot, qoh = _NO_ROWS if q is None else _rope_rows(q, q_out, "q", geom.Hq, B, packed, device)
+    Tk, k_out, k0, kb, kt, kh, ko0, kob, kot, koh = _NO_ROWS if k is None else _rope_rows(k, k_out, "k", geom.Hkv, B, packed, device)
+    if q is None:
+        T = Tk
+    elif k is not None and (T != Tk or q.dim() != k.dim()):
         raise ValueError("q and k must have the same rows")
     if packed:
-        R = geom.B
         if ctx_len is None:
             raise ValueError("q_start needs ctx_len")
-        if (q_start.dtype is not _INT or ctx_len.dtype is not _INT or q_start.shape != (R + 1,) or ctx_len.shape != (R,)
+        if (q_start.dtype is not _INT or ctx_len.dtype is not _INT or q_start.shape != (B + 1,) or ctx_len.shape != (B,)
                 or not (q_start.is_contiguous() and ctx_len.is_contiguous())):
-            _ints(q_start, "q_start", (R + 1,))
-            _ints(ctx_len, "ctx_len", (R,))
+            _ints(q_start, "q_start", (B + 1,))
+            _ints(ctx_len, "ctx_len", (B,))
     if pos is not None:
-        _ints(pos, "pos", (T,) if first.dim() == 3 else (geom.B, T))
-    device = first.get_device()
-    _on(device, q, k, freqs, pos, q_start, ctx_len)
-    _run(load_library().antkv_rope, "antkv_rope", device, geom._c, *qs[:4], *ks[:4], T, _p(pos), _p(q_start), _p(ctx_len), pos0, freqs.data_ptr(), 2 * rot[0],
-         style, amplitude, inverse, *qs[4:], *ks[4:], _stream(first))
+        _ints(pos, "pos", (T,) if first.dim() == 3 else (B, T))
+    _on(device, freqs, q_start, ctx_len, pos)
+    _run(load_library().antkv_rope, "antkv_rope", device, geom._c, q0, qb, qt, qh, k0, kb, kt, kh, T, _p(pos), _p(q_start), _p(ctx_len), pos0, freqs.data_ptr(),
+         2 * rot[0], style, amplitude, inverse, qo0, qob, qot, qoh, ko0, kob, kot, koh, _stream(first))
     return q_out, k_out
