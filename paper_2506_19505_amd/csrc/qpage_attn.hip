@@ -294,7 +294,7 @@ struct BytePages {
         };
         const Operands at(lds0, lds0 + 2 * kTileBytes, lane);
         half8_t tq[8], pr[2][2];
-        load_query(tq, p, x, row, lane);
+        load_query<false, false>(tq, p, x, row, lane);              // on its way under the first look at the pages
         float16_t sc[2];
         auto place_at = [&](int tile, int j) {                      // of 16-key half j, -1: no page
             int key = tile * 32 + 16 * j;
@@ -329,6 +329,8 @@ struct BytePages {
             // the V slot of "tile -1" is multiplied with zero probabilities: it has to be finite
 #pragma unroll
             for (int i = 0; i < 8 / NW; ++i) *(uint4_t*)(s_kv + 3 * kTileBytes + (i * NW * 64 + tid) * 16) = uint4_t{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int s = 0; s < 8; ++s) pin(tq[s]);
             wait_all_loads();
             __syncthreads();
             auto own_place = [&](int i) { return scalar(notes[i].place[half]); };

@@ -282,15 +282,17 @@ __device__ __forceinline__ void add_odd(Sums& x, const At& at, int slot, uint32_
 
 // The query row of each lane (row n of the tile that starts at row w_row; rows behind the last repeat it).  k-step s takes channels 16 s + 8 kh
 // .. + 7; kPairs: 32 (s / 2) + 16 kh + 8 (s % 2) .. + 7, so that two steps of an operand of K are 16 channels in a row
-template <bool kPairs = false>
+template <bool kPairs = false, bool kPin = true>
 __device__ __forceinline__ void load_query(half8_t (&tq)[8], const Params& p, const Piece& x, int row, int lane)
 {
     const int tok = row >> p.gs, h = (x.g << p.gs) + (row & (p.G - 1));
     const half_t* qp = p.q + x.b * p.qs_b + (int64_t)(x.rq.t0 + tok) * p.qs_t + h * p.qs_h + (kPairs ? 16 : 8) * (lane >> 5);
 #pragma unroll
     for (int s = 0; s < 8; ++s) tq[s] = *(const half8_t*)(qp + (kPairs ? 32 * (s >> 1) + 8 * (s & 1) : 16 * s));
+    if (kPin) {                                                     // (which waits for them)
 #pragma unroll
-    for (int s = 0; s < 8; ++s) pin(tq[s]);
+        for (int s = 0; s < 8; ++s) pin(tq[s]);
+    }
 }
 
 // Softmax of a tile's scores s, whose probabilities are then in `now`, with the scores y of the tile in K slot `next` and the value product of
