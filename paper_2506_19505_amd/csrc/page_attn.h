@@ -135,11 +135,12 @@ __device__ __forceinline__ bool last_to_arrive(unsigned long long* word, uint64_
 __device__ __forceinline__ float weight(float from, float to) { return fmaxf(fast_exp2(from - to), 1.17549435e-38f); }
 
 // Adds the partial sums of a row of a narrow block: a wave, two channels to a lane.
+template <class Cache>
 __device__ __forceinline__ void merge_row(const Params& p, const Pieces& pc, int row, int g, int64_t t, int h, int lane)
 {
     const int S = pc.last - pc.first + 1;
     auto at = [&](int s) { return pc.slot(p, pc.first + s, g) * p.rows_cap + row; };
-    constexpr int kBatch = 16;
+    constexpr int kBatch = Cache::kBatch;
     float m = kNegBig, s_max = kMasked, l = 0.f, o0 = 0.f, o1 = 0.f;
     for (int s0 = 0; s0 < S; s0 += 64) {                            // lane: piece s0 + lane
         float2_t x = {kNegBig, 0.f}, y = {kMasked, 0.f};
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
     int size = 1, x = share, end = total;                           // the share: costs x .. end - 1 (unit: block x)
     if (!p.unit) {
         size = (total + p.shares - 1) / p.shares;
-        const int least = wide ? Cache::kLeastWide : Cache::kLeastNarrow;       // less is not worth the partial sums
+        const int least = Cache::least(wide, total);                // less is not worth the partial sums
         if (size < least) size = least;
         x = share < p.shares ? share * size : total;
         end = x + size < total ? x + size : total;
@@ -341,7 +342,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
         }
         if (some) {
             const int pieces = all.last - all.first + 1;
-            unsigned long long* word = p.done + (int64_t)all.last * p.Hkv + g;
+            unsigned long long* word = p.done + ((int64_t)all.last * p.Hkv + g) * Cache::kWordApart;
             unsigned long long seen = 0;
             if (pieces > 1 && tid == 0) seen = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             Sums sums;
@@ -404,7 +405,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
                     }
                 }
                 if (pieces > 1 && last_to_arrive(word, p.tag, pieces, &s_flag))
-                    for (int row = wave; row < rows; row += NW) merge_row(p, all, row, g, rq.t0 + (row >> p.gs), (g << p.gs) + (row & (p.G - 1)), lane);
+                    for (int row = wave; row < rows; row += NW) merge_row<Cache>(p, all, row, g, rq.t0 + (row >> p.gs), (g << p.gs) + (row & (p.G - 1)), lane);
             } else {
                 Cache::template wide_sums<NW>(sums, p, pc, span, s_all + At::tiles, &s_odd, s_notes);
                 claim();
@@ -451,12 +452,13 @@ inline bool unit_blocks(const Geom& g, int64_t T, int64_t most, int64_t longest)
 }
 
 // What either would need: a workspace made for many tokens then does for fewer.
+template <class Cache>
 inline size_t workspace_bytes(const Geom& g, int64_t T)
 {
     size_t most = 0;
     for (int nw = 4; nw <= 8; nw += 4) {
         const size_t pairs = (size_t)shares_of(g, nw) * g.Hkv;
-        const size_t n = align_up(pairs * sizeof(unsigned long long)) + 2 * pairs * rows_cap_of(g, T, nw) * (kD + 4) * sizeof(float);
+        const size_t n = align_up(pairs * sizeof(unsigned long long) * Cache::kWordApart) + 2 * pairs * rows_cap_of(g, T, nw) * (kD + 4) * sizeof(float);
         most = most < n ? n : most;
     }
     return most;
@@ -470,7 +472,7 @@ inline hipError_t launch_waves(const Geom& g, Params& p, int64_t T, void* ws, hi
     const int64_t pairs = (int64_t)p.shares * g.Hkv;
     p.tag = next_launch_tag();
     p.done = (unsigned long long*)ws;
-    p.part_out = (float*)((char*)ws + align_up((size_t)pairs * sizeof(unsigned long long)));
+    p.part_out = (float*)((char*)ws + align_up((size_t)pairs * sizeof(unsigned long long) * Cache::kWordApart));
     p.part_stat = p.part_out + 2 * pairs * p.rows_cap * kD;
     const int64_t most = T * g.G / (32 * NW) + (g.B < T ? g.B : T);         // blocks that there can be
     p.unit = unit_blocks<Cache>(g, T, most, p.table_cap << p.shift);

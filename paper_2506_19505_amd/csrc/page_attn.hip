@@ -22,7 +22,9 @@ struct Fp16Pages {
     static constexpr int kIdleNarrow = 14, kIdleWide = 16;
     // The smallest shares.  8, 12, 16: a token on 4096 keys 14.7, 13.2, 13.8 us, one each of 4 requests on 2048 keys 16.6, 14.5, 14.9; 16, 24, 32: 64
     // tokens on 4096 keys 32.5, 33.9, 36.0, 300 on 2000 39.4, 38.1, 46.2, 4 x 100 on 1000 32.1, 31.4, 32.0
-    static constexpr int kLeastNarrow = 12, kLeastWide = 24;
+    __device__ __forceinline__ static int least(bool wide, int) { return wide ? 24 : 12; }
+    static constexpr int kWordApart = 1;                            // arrival words: 8 bytes apart
+    static constexpr int kBatch = 16;                               // partial sums of a row that are asked for together
     static constexpr int kFirst = 4;                                // key tiles of a block's first piece, at least
     static constexpr int kRowsOfEight = 1024;                       // of a request on average, and a KV head: for workgroups of eight waves
 
@@ -184,7 +186,7 @@ struct Fp16Pages {
 };
 }  // namespace
 
-size_t page_attn_workspace_bytes(const Geom& g, int64_t T) { return paged::workspace_bytes(g, T); }
+size_t page_attn_workspace_bytes(const Geom& g, int64_t T) { return paged::workspace_bytes<Fp16Pages>(g, T); }
 
 hipError_t launch_page_attn(const Geom& g, const Pages& pg, const PageAttnArgs& a, void* ws, hipStream_t st) { return paged::launch<Fp16Pages>(g, pg, a, ws, st); }
 

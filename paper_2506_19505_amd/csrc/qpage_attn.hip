@@ -67,10 +67,17 @@ struct BytePages {
     static constexpr int kShiftNarrow = 1, kShiftWide = 2;
     // Of coming and going: 10 and 15 us a block (pages, scales, first tiles 5, partial sums 4).  Narrow, 32 and 40: 64 tokens on 1 .. 32768 keys 88 and 85 us
     static constexpr int kIdleNarrow = 40, kIdleWide = 64;
-    // The smallest shares.  24 and 36: a token on 4096 keys 12.5 and 13.5 us; 96 and 144: 300 tokens on 2000 keys 42 and 52
-    static constexpr int kLeastNarrow = 24, kLeastWide = 96;
+    // The smallest shares.  Narrow blocks, 20, 24, 32, 40: a token on 1024 keys 11.3, 11.9, 12.0, 12.6 us, on 4096 12.1, 12.5, 12.7, 12.8, but on 16384 20.5, 20.0, 17.7, 17.0
+    // (each piece arrives at the same word, and is asked for by the last one), 16 on 300 each 10.5, 11.7, 11.1, 10.6, 4 on 2048 13.5, 13.3, 13.7, 13.8.
+    // Wide ones, 96 and 144: 300 tokens on 2000 keys 42 and 52
+    __device__ __forceinline__ static int least(bool wide, int total) { return wide ? 96 : total < 480 ? 20 : 32; }
     // Key tiles of a block's first piece, at least.  4 and 8: 16 tokens on 300 keys each 13.6 and 12.7 us, 4 x 100 on 1000 36.3 and 34.9
     static constexpr int kFirst = 8;
+    // Partial sums of a row that are asked for together (more are padded).  8, 12, 16, 32: 40 single tokens on 300 keys 11.2, 11.5, 11.9, 13.3 us, one on 4096 12.3, 12.0,
+    // 12.3, 14.0, on 16384 22.7, 22.5, 22.8, 24.1
+    static constexpr int kBatch = 8;
+    // Arrival words, in 8 bytes apart.  1 and 16, a line each: a token on 32768 keys 31.3 and 25.2 us, on 16384 22.7 and 20.0, on 4096 12.3 and 12.5
+    static constexpr int kWordApart = 16;
     // 1024 and 512: 16 requests with 2048 tokens among them 88 and 102 us; 1024 and 256: 64 tokens on 4096 keys 39 and 50
     static constexpr int kRowsOfEight = 1024;
 
@@ -469,7 +476,7 @@ struct BytePages {
 
 }  // namespace
 
-size_t qpage_attn_workspace_bytes(const Geom& g, int64_t T) { return paged::workspace_bytes(g, T); }
+size_t qpage_attn_workspace_bytes(const Geom& g, int64_t T) { return paged::workspace_bytes<BytePages>(g, T); }
 
 hipError_t launch_qpage_attn(const Geom& g, const Pages& pg, const PageAttnArgs& a, void* ws, hipStream_t st) { return paged::launch<BytePages>(g, pg, a, ws, st); }
 
