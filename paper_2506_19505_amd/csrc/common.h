@@ -200,6 +200,7 @@ struct PageAttnArgs {
 };
 size_t page_attn_workspace_bytes(const Geom& g, int64_t T);
 hipError_t launch_page_attn(const Geom& g, const Pages& pg, const PageAttnArgs& a, void* ws, hipStream_t st);
+
 // q or k of a call on rotary positions: [B][T][heads][D] with strides in elements, channel stride 1
 struct RopeRows {
     const half_t* x;

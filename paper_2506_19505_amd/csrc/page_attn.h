@@ -427,7 +427,7 @@ __global__ __launch_bounds__(NW * 64, 2) void page_attn_kernel(const Params p)
 }
 
 // Long chunks: 8 waves read a key tile for 256 rows; fewer tokens: 4 waves, two workgroups to a CU, one works while the other comes or
-// goes.  With 8 and 4 waves, 32 heads on 8: a chunk of 2048 on 32768 keys 998 and 1125 us, 8192 on 32768 3510 and 3645, 8 prompts of 1024 120 and 127,
+// goes.  With 8 and 4 waves, FP16 pages, 32 heads on 8: a chunk of 2048 on 32768 keys 998 and 1125 us, 8192 on 32768 3510 and 3645, 8 prompts of 1024 120 and 127,
 // 64 of 256 154 and 147, one of 300 on 2000 keys 38 and 35; 4 of 100 on 1000 38 and 32, 64 tokens on 4096 keys 45 and 34, 16 requests with 2048 tokens
 // among them (500 for four of them, one for the others) on up to 8192 keys 93 and 83, one token on 4096 14.5 and 13.2.
 // The lengths are on the device, so that the host goes by the mean.  One long chunk among many short requests is on the slower side then, 2048 tokens on
@@ -441,7 +441,7 @@ inline int shares_of(const Geom& g, int nw) { return g.Hkv < kWaves / nw ? kWave
 inline int rows_cap_of(const Geom& g, int64_t T, int nw) { return T * g.G < 32 * nw ? ((int)(T * g.G) + 31) / 32 * 32 : 32 * nw; }
 
 // A workgroup per block, where prompts are long and blocks two to a workgroup at least, so that nothing has to be cut: blocks of a prompt
-// that run at the same time are then on about the same keys, which come out of the L2.  In shares and in blocks, 32 heads on 8: 16384
+// that run at the same time are then on about the same keys, which come out of the L2.  In shares and in blocks, FP16 pages, 32 heads on 8: 16384
 // tokens 2108 and 2067 us, 8192 on 32768 keys 3618 and 3510, 4 x 4096 616 and 595, 8 x 2048 369 and 350, 4 x 2048 on 2048 .. 16384 834 and 789, but
 // 8 x 1024 123 and 132, 1000 x 100 838 and 1201, 4096 tokens on 100 keys each 539 and 1540.  Also where the costs of all blocks might not
 // fit an int.

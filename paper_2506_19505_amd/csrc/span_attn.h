@@ -58,7 +58,7 @@ struct Params {
     int T, R, shift;
     int shares, rows_cap;                                           // shares of the work per KV head; rows of a piece's partial sums
     int unit;                                                       // a workgroup per block instead of per share
-    unsigned long long* done;                                       // [shares][Hkv] arrival words (launch_tag.h) of the blocks that end there
+    unsigned long long* done;                                       // [shares][Hkv] arrival words (launch_tag.h), Cache::kWordApart apart, of the blocks that end there
     uint64_t tag;
     float *part_out, *part_stat;                                    // [2 shares][Hkv][rows_cap] x D sums, x 4: reference, sum, largest score
     const float *k_scales, *v_scales;                               // pages of 8 bits: of every 16 tokens of a head
