@@ -790,10 +790,13 @@ def rope(geom: Geometry, q: torch.Tensor | None, k: torch.Tensor | None, freqs: 
     """antkv_rope: q fp16 [T,Hq,D] and k [T,Hkv,D] of a packed batch (with q_start int32 [B+1] and ctx_len int32 [B], as page_map makes them) or of one
     sequence, or [B,Hq,T,D] and [B,Hkv,T,D]; positions pos (int32, [T] or [B,T]) or pos0, pos0 + 1, ..; freqs fp64 [rot_dim/2] (rope_freqs) ->
     (q_out, k_out), made here where they are not given; q_out=q turns q in place.  Rows outside a packed batch's requests are left as they
-    are (undefined where the output is made here)."""
+    are (undefined where the output is made here).  Records no gradient, and refuses rows that ask for one: that of a call is the same call with
+    `inverse` the other way round, of the gradients of its outputs."""
     first = k if q is None else q
     if first is None:
         raise ValueError("q or k must be given")
+    if (first.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
+        raise ValueError("rope records no gradient: call it under torch.no_grad(), and with the other `inverse` for the gradient")
     packed, device, B = q_start is not None, first.get_device(), geom.B
     rot = freqs.shape
     if freqs.dtype is not torch.float64 or len(rot) != 1 or not freqs.is_contiguous():
