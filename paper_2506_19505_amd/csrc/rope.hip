@@ -17,7 +17,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnits = kD / 16;                                     // threads of a head's row
 constexpr int kPass = kThreads / kUnits;                            // rows of a pass
-constexpr int kAhead = 1;                                           // rows of a thread whose loads are in flight together
 constexpr int kTokens = 32;                                         // of a workgroup, at most
 constexpr int64_t kCaches = 32LL << 20;                             // bytes of the eight L2s
 constexpr int kMostGroups = 1 << 20;
@@ -51,26 +50,6 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs p, int to
     const int rows = tokens * H;
     for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
         const int64_t first = group * tokens;                       // token of all B x T
-        uint4_t x[kAhead], y[kAhead];
-        uint4_t* to[kAhead];
-        int at[kAhead];
-        auto load = [&](int row0) __attribute__((always_inline)) {
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const int row = row0 + j * kPass, i = row / H, h = row - i * H;
-                to[j] = nullptr;
-                at[j] = i;
-                if (row < rows && first + i < p.B * p.T) {
-                    const uint32_t u = (uint32_t)(first + i), n = p.B > 1 ? u / (uint32_t)p.T : 0, t = u - n * (uint32_t)p.T;
-                    const RopeRows& z = h < p.Hq ? p.q : p.k;
-                    const int hh = h < p.Hq ? h : h - p.Hq;
-                    const uint4_t* from = (const uint4_t*)(z.x + n * z.xs_b + t * z.xs_t + hh * z.xs_h);
-                    to[j] = (uint4_t*)(z.y + n * z.ys_b + t * z.ys_t + hh * z.ys_h);
-                    x[j] = from[a];
-                    y[j] = from[b];
-                }
-            }
-        };
         if (group != blockIdx.x) __syncthreads();
         for (int i = wave; i < tokens; i += kThreads / 64) {
             const int64_t u = first + i;
@@ -93,46 +72,59 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs p, int to
             if (lane == 0) s_live[i] = live;
         }
         __syncthreads();
-        for (int row0 = tid / kUnits; row0 < rows; row0 += kAhead * kPass) {
-            load(row0);
+        for (int row = tid / kUnits; row < rows; row += kPass) {
+            const int i = row / H, h = row - i * H;
+            uint4_t x, y;
+            uint4_t* to = nullptr;
+            if (first + i < p.B * p.T) {                            // asked for before it is known whether the row is somebody's
+                // (values are selected: a selected address is loaded through, a chain of its own in front of the row, 32768 tokens 119 -> 127 us)
+                const uint32_t u = (uint32_t)(first + i), n = p.B > 1 ? u / (uint32_t)p.T : 0, t = u - n * (uint32_t)p.T;
+                const bool of_q = h < p.Hq;
+                const int hh = of_q ? h : h - p.Hq;
+                const half_t* from_rows = of_q ? p.q.x : p.k.x;
+                half_t* to_rows = of_q ? p.q.y : p.k.y;
+                const int64_t xs_b = of_q ? p.q.xs_b : p.k.xs_b, xs_t = of_q ? p.q.xs_t : p.k.xs_t, xs_h = of_q ? p.q.xs_h : p.k.xs_h;
+                const int64_t ys_b = of_q ? p.q.ys_b : p.k.ys_b, ys_t = of_q ? p.q.ys_t : p.k.ys_t, ys_h = of_q ? p.q.ys_h : p.k.ys_h;
+                const uint4_t* from = (const uint4_t*)(from_rows + n * xs_b + t * xs_t + hh * xs_h);
+                to = (uint4_t*)(to_rows + n * ys_b + t * ys_t + hh * ys_h);
+                x = from[a];
+                y = from[b];
+            }
+            if (!to || !s_live[i]) continue;
+            if (turns) {
+                const float4_t* cs = (const float4_t*)&s_turn[i][8 * unit];
+                float c[8], s[8];
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j)
-                if (to[j] && s_live[at[j]]) {
-                    if (turns) {
-                        const float4_t* cs = (const float4_t*)&s_turn[at[j]][8 * unit];
-                        float c[8], s[8];
+                for (int e = 0; e < 8; ++e) {
+                    c[e] = cs[e >> 1][2 * (e & 1)];
+                    s[e] = cs[e >> 1][2 * (e & 1) + 1];
+                }
+                half8_t u = __builtin_bit_cast(half8_t, x), w = __builtin_bit_cast(half8_t, y), yu, yw;
+                if (p.style == 1) {                                 // pair e: channel e of either piece
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            c[e] = cs[e >> 1][2 * (e & 1)];
-                            s[e] = cs[e >> 1][2 * (e & 1) + 1];
-                        }
-                        half8_t u = __builtin_bit_cast(half8_t, x[j]), w = __builtin_bit_cast(half8_t, y[j]), yu, yw;
-                        if (p.style == 1) {                         // pair e: channel e of either piece
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                yu[e] = (half_t)((float)u[e] * c[e] - (float)w[e] * s[e]);
-                                yw[e] = (half_t)((float)w[e] * c[e] + (float)u[e] * s[e]);
-                            }
-                        } else {                                    // pair e: channels 2 e, 2 e + 1 of the sixteen
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                yu[2 * e] = (half_t)((float)u[2 * e] * c[e] - (float)u[2 * e + 1] * s[e]);
-                                yu[2 * e + 1] = (half_t)((float)u[2 * e + 1] * c[e] + (float)u[2 * e] * s[e]);
-                                yw[2 * e] = (half_t)((float)w[2 * e] * c[4 + e] - (float)w[2 * e + 1] * s[4 + e]);
-                                yw[2 * e + 1] = (half_t)((float)w[2 * e + 1] * c[4 + e] + (float)w[2 * e] * s[4 + e]);
-                            }
-                        }
-                        x[j] = __builtin_bit_cast(uint4_t, yu);
-                        y[j] = __builtin_bit_cast(uint4_t, yw);
+                    for (int e = 0; e < 8; ++e) {
+                        yu[e] = (half_t)((float)u[e] * c[e] - (float)w[e] * s[e]);
+                        yw[e] = (half_t)((float)w[e] * c[e] + (float)u[e] * s[e]);
                     }
-                    if (kStream) {
-                        __builtin_nontemporal_store(x[j], to[j] + a);
-                        __builtin_nontemporal_store(y[j], to[j] + b);
-                    } else {
-                        to[j][a] = x[j];
-                        to[j][b] = y[j];
+                } else {                                            // pair e: channels 2 e, 2 e + 1 of the sixteen
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        yu[2 * e] = (half_t)((float)u[2 * e] * c[e] - (float)u[2 * e + 1] * s[e]);
+                        yu[2 * e + 1] = (half_t)((float)u[2 * e + 1] * c[e] + (float)u[2 * e] * s[e]);
+                        yw[2 * e] = (half_t)((float)w[2 * e] * c[4 + e] - (float)w[2 * e + 1] * s[4 + e]);
+                        yw[2 * e + 1] = (half_t)((float)w[2 * e + 1] * c[4 + e] + (float)w[2 * e] * s[4 + e]);
                     }
                 }
+                x = __builtin_bit_cast(uint4_t, yu);
+                y = __builtin_bit_cast(uint4_t, yw);
+            }
+            if (kStream) {
+                __builtin_nontemporal_store(x, to + a);
+                __builtin_nontemporal_store(y, to + b);
+            } else {
+                to[a] = x;
+                to[b] = y;
+            }
         }
     }
 }
@@ -159,7 +151,7 @@ hipError_t launch_rope(const RopeArgs& a, hipStream_t st)
     // A workgroup's tokens: those of one pass, fewer where that leaves CUs without a workgroup.  One, two and four rows of a thread in flight, 32768
     // tokens of 40 heads 124, 125 and 129 us, of 8 heads 32, 34 and 37; workgroups of twice the size, one row, 157 and 35; loads ahead of the angles (more
     // registers, fewer waves) 147 and 37.
-    int tokens = kAhead * kPass / H;
+    int tokens = kPass / H;
     tokens = tokens < 1 ? 1 : tokens < kTokens ? tokens : kTokens;
     while (tokens > 1 && all / tokens < 1024) tokens /= 2;
     const int64_t groups = (all + tokens - 1) / tokens;
