@@ -100,3 +100,21 @@ def test_rows_of_blocks_between_each_other(T, Hkv):
         rng.shuffle(again[a:a + 16])
     pools.store(geometry(Hkv), v, k * 20, again.tolist())
     pools.check("second")
+
+
+@pytest.mark.parametrize("new", [1, 8, 300])
+def test_scales_that_are_no_powers_of_two(new):
+    """Loading and attention take a positive normal scale for the power of two at or below it, in narrow blocks and in wide ones, bit for bit."""
+    Hq, Hkv, page, n = 8, 2, 32, 700
+    gen, geom = gen_of(new), antkv.Geometry(1, Hq, Hkv, 8)
+    q = randn(gen, new, Hq, D)
+    pools = Pools(24, Hkv, page, seed=new)
+    table = torch.randperm(24, device="cuda", generator=gen).to(torch.int32)[None]
+    even = [s.clone() for s in pools.scales]
+    for s in pools.scales:                                          # 1.0 to 1.99 of them
+        s.mul_(1 + 0.99 * torch.rand(s.shape, device="cuda", generator=gen))
+    args = lambda scales: (*pools.bytes, *scales)
+    starts, ctx = torch.tensor([0, new], dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda")
+    want, got = ((*antkv.qpage_load(geom, *args(s), table, n), *antkv.qpage_attn(geom, q, 0.001, starts, ctx, table, *args(s), want_stats=True)) for s in (even, pools.scales))
+    assert all(x.isfinite().all() for x in want)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
