@@ -69,7 +69,10 @@ struct BytePages {
     static constexpr int kIdleNarrow = 40, kIdleWide = 64;
     // The smallest shares.  Narrow blocks, 20, 24, 32, 40: a token on 1024 keys 11.3, 11.9, 12.0, 12.6 us, on 4096 12.1, 12.5, 12.7, 12.8, but on 16384 20.5, 20.0, 17.7, 17.0
     // (each piece arrives at the same word, and is asked for by the last one), 16 on 300 each 10.5, 11.7, 11.1, 10.6, 4 on 2048 13.5, 13.3, 13.7, 13.8.
-    // Wide ones, 96 and 144: 300 tokens on 2000 keys 42 and 52
+    // Wide ones, 96 and 144: 300 tokens on 2000 keys 42 and 52.  All of these are of 32 heads on 8, 64 shares of a KV head.  Of 32 on 32, 16 shares, narrow 20, 32, 40: a
+    // token on 1024 keys 11.4, 12.0, 12.6, on 4096 16.7, 15.6, 14.8 (12 % that the rule leaves there), on 16384 34.9 and on 32768 57.5 with any; wide 48, 96, 144: 300 on 2000
+    // 38, 35, 43, 4 x 100 on 1000 32.9, 33.8, 37.3.  The rules around this one make no difference there (1 % at most, from kFirst 4, kIdleNarrow 32, words 8 bytes
+    // apart, kRowsOfEight 512)
     __device__ __forceinline__ static int least(bool wide, int total) { return wide ? 96 : total < 480 ? 20 : 32; }
     // Key tiles of a block's first piece, at least.  4 and 8: 16 tokens on 300 keys each 13.6 and 12.7 us, 4 x 100 on 1000 36.3 and 34.9
     static constexpr int kFirst = 8;

@@ -6,8 +6,8 @@
 // touch the same block: nothing is waited for and nothing is atomic.
 // A wave looks at `span` rows of the batch for the first rows of blocks: 16 in long batches (about one block), 1 in short ones, where each row may
 // be a request of its own.
-// Bound: HBM in long batches (32768 tokens of 8 heads 42.5 us, 4.7 TB/s read and written), in short ones a chain of slot - rows and scale - bytes (64 tokens
-// 3.9 us).
+// Bound: HBM in long batches (32768 tokens of 8 heads 42.5 us, 4.7 TB/s read and written); in short ones (64 tokens of 64 requests 4.0 us a call in a captured loop,
+// 4.5 in a trace) a chain: slots, rows, then K's scale (behind the rows' largest value, and only where the block goes on) and K's bytes, then V's scale and bytes.
 //
 // Loading is a copy: 8 bytes in, 16 out per lane, 16 lanes to a row, K and V by the same thread.  Bound: HBM.
 #include "bytes.h"
@@ -234,7 +234,9 @@ __global__ __launch_bounds__(kThreads) void qpage_load_kernel(const uint2_t* __r
 int units_of(int Hkv) { return (Hkv + kWavesOf - 1) / kWavesOf; }
 // A wave goes through its blocks one after the other, 1.6 us each: a step of single tokens has one for every row, a prompt one for 16.  Spans
 // of 1, 2, 8 and 16, 8 heads, a prompt and as many requests of a token: 500 tokens 5.1, 4.6, 3.7, 5.1 us and 5.2, 6.2, 15, 27; 1024 8.6, 6.3, 5.6, 4.9
-// and 7.8, 7.5, 15, 28; 2048 14, 9.6, 6.9, 5.7 and 13, 12, 17, 29; 4096 25, 16, 8.5, 7.6 and 23, 21, 22, 32; 32768 (a prompt) 246, 135, 49, 42
+// and 7.8, 7.5, 15, 28; 2048 14, 9.6, 6.9, 5.7 and 13, 12, 17, 29; 4096 25, 16, 8.5, 7.6 and 23, 21, 22, 32; 32768 (a prompt) 246, 135, 49, 42.
+// 32 heads: 128 tokens 4.6, 3.8, 5.0, 5.0 and 5.2, 6.2, 15, 28; 512 7.7, 6.6, 5.9, 5.8 and 13, 13, 18, 30; 1024 12.6, 10.5, 7.3, 7.9 and 23, 22, 22, 34; 4096 50, 44, 25,
+// 20 and 90, 80, 82, 86; 32768 376, 324, 177, 154
 int span_of(int64_t T, int Hkv)
 {
     const int64_t n = T * units_of(Hkv);

@@ -7,7 +7,9 @@
 // A workgroup takes a few tokens with all of their heads.  A wave works out a token's 64 angles, one to a lane: the product with the position
 // and its reduction to a turn in fp64 (far positions turn thousands of times: fp32 would leave an error of 0.01 at 10^5), then sine and cosine
 // in fp32, and leaves them in LDS.  A thread turns 16 channels (eight pairs) of a head: 32 bytes in, 32 out, fp32 in between, rounded once.
-// Bound: HBM in long batches (32768 tokens of 40 heads 118 us, 5.7 TB/s read and written), launch and two dependent loads in short ones (64 tokens 3.7).
+// Bound: HBM in long batches (32768 tokens of 40 heads 119 us, 5.7 TB/s read and written); in short ones (64 tokens of 64 requests 3.8 us a call in a captured
+// loop, 4.4 in a trace) the launch and five loads one behind the other: the search of q_start, the request's two starts, its length, the frequency and, behind
+// the barrier, the rows.  The frequency and the rows need none of the others.
 #include "common.h"
 
 namespace antkv {
@@ -150,7 +152,7 @@ hipError_t launch_rope(const RopeArgs& a, hipStream_t st)
     const int64_t all = a.B * a.T;
     // A workgroup's tokens: those of one pass, fewer where that leaves CUs without a workgroup.  One, two and four rows of a thread in flight, 32768
     // tokens of 40 heads 124, 125 and 129 us, of 8 heads 32, 34 and 37; workgroups of twice the size, one row, 157 and 35; loads ahead of the angles (more
-    // registers, fewer waves) 147 and 37.
+    // registers, fewer waves) 147 and 37 (not tried on short batches alone, where no waves are missing).
     int tokens = kPass / H;
     tokens = tokens < 1 ? 1 : tokens < kTokens ? tokens : kTokens;
     while (tokens > 1 && all / tokens < 1024) tokens /= 2;
